@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libtdc.so, with the same names as ``include/tdc.h``.
+"""Thin ctypes binding of libtdc.so, with the same names as ``include/tdc.h``, ``tdc_norm.h`` and ``tdc_mx4.h``.
 
 Argument marshalling only: every step of the layer runs in the library's HIP
 kernels.  PyTorch is used for device memory and streams.  There is no CPU
@@ -33,13 +33,21 @@ VARIANT_NAMES = {0: "auto", 1: "naive", 2: "split", 3: "fused", 4: "chain", 5: "
                  8: "merged_xcd"}
 ERR_WAIT = -10
 
-# every symbol include/tdc.h declares
+F32, F16, BF16 = 0, 1, 2                       # element types of activations (tdc_norm.h)
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU}
+
+# every symbol the headers declare
 EXPORTS = ["tdc_plan_create", "tdc_plan_create_tuned", "tdc_plan_pack_weights", "tdc_conv_tucker2",
            "tdc_plan_destroy", "tdc_plan_get_tuning", "tdc_plan_describe", "tdc_plan_workspace_bytes",
            "tdc_plan_kernel_count", "tdc_status_string", "tdc_version", "tdc_out_size",
            "tdc_select_tuning", "tdc_launch_null", "tdc_plan_pack_dense", "tdc_conv_dense", "tdc_select_ranks",
            "tdc_conv_tucker2_ex", "tdc_conv_dense_ex", "tdc_hosvd_tucker2", "tdc_admm_project",
-           "tdc_conv_tucker2_static", "tdc_model_terms", "tdc_plan_status", "tdc_plan_set_wait_limit", "tdc_plan_waits_given_up"]
+           "tdc_conv_tucker2_static", "tdc_model_terms", "tdc_plan_status", "tdc_plan_set_wait_limit", "tdc_plan_waits_given_up",
+           "tdc_norm_plan_create", "tdc_norm_plan_destroy", "tdc_norm_plan_workspace_bytes", "tdc_norm_plan_kernel_count",
+           "tdc_group_norm", "tdc_group_norm_mx4", "tdc_group_norm_backward",
+           "tdc_mx4_quantize", "tdc_mx4_dequantize", "tdc_mx4_matmul", "tdc_mx4_plan_create", "tdc_mx4_plan_destroy",
+           "tdc_mx4_plan_workspace_bytes", "tdc_mx4_plan_kernel_count", "tdc_mx4_plan_pack", "tdc_conv_mx4", "tdc_conv_mx4_quantized"]
 
 
 class tdc_shape(ctypes.Structure):
@@ -72,6 +80,28 @@ class tdc_rank_choice(ctypes.Structure):
 
 class tdc_epilogue(ctypes.Structure):
     _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("relu", ctypes.c_int32)]
+
+
+class tdc_norm_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "H", "W", "C", "groups", "dtype", "act")] + [("eps", ctypes.c_float)]
+
+
+class tdc_norm_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("residual", "mean", "rstd")] +
+                [(n, ctypes.c_int64) for n in ("x_pitch", "residual_pitch", "y_pitch")])
+
+
+class tdc_norm_grad_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("residual", "dresidual")] +
+                [(n, ctypes.c_int64) for n in ("x_pitch", "residual_pitch", "dy_pitch", "dx_pitch", "dresidual_pitch")])
+
+
+class tdc_mx4_epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("act", ctypes.c_int32)]
+
+
+class tdc_mx4_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "H", "W", "C", "N", "stride", "dtype")] + [("x_pitch", ctypes.c_int64)]
 
 
 class TdcError(RuntimeError):
@@ -151,6 +181,21 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.tdc_hosvd_tucker2.restype = ip
     lib.tdc_admm_project.argtypes = [fp, fp, ip, ip, ip, ip, ip, fp]
     lib.tdc_admm_project.restype = ip
+    i64 = ctypes.c_int64
+    norm_shape, mx4_shape = ctypes.POINTER(tdc_norm_shape), ctypes.POINTER(tdc_mx4_shape)
+    norm_args, grad_args, mx4_epi = ctypes.POINTER(tdc_norm_args), ctypes.POINTER(tdc_norm_grad_args), ctypes.POINTER(tdc_mx4_epilogue)
+    for name, args in (("tdc_norm_plan_create", [ctypes.POINTER(vp), norm_shape, ip]), ("tdc_norm_plan_destroy", [vp]), ("tdc_norm_plan_kernel_count", [vp]),
+                       ("tdc_group_norm", [vp] * 6 + [norm_args]), ("tdc_group_norm_mx4", [vp] * 7 + [norm_args]),
+                       ("tdc_group_norm_backward", [vp] * 11 + [grad_args]),
+                       ("tdc_mx4_quantize", [vp, vp, ip, i64, i64, i64, vp, vp]), ("tdc_mx4_dequantize", [vp, vp, vp, i64, i64, vp, ip, i64]),
+                       ("tdc_mx4_matmul", [vp] * 5 + [ctypes.c_int32] * 3 + [vp, ip, mx4_epi]),
+                       ("tdc_mx4_plan_create", [ctypes.POINTER(vp), mx4_shape, ip]), ("tdc_mx4_plan_destroy", [vp]), ("tdc_mx4_plan_kernel_count", [vp]),
+                       ("tdc_mx4_plan_pack", [vp, vp, vp]), ("tdc_conv_mx4", [vp, vp, vp, vp, mx4_epi]), ("tdc_conv_mx4_quantized", [vp] * 5 + [mx4_epi])):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, ip
+    for name in ("tdc_norm_plan_workspace_bytes", "tdc_mx4_plan_workspace_bytes"):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = [vp], ctypes.c_size_t
     if path is None:
         _lib = lib
     return lib
@@ -410,3 +455,101 @@ def tdc_admm_project(K_weights, M, R1: int, R2: int):
     if rc != TDC_OK:
         raise TdcError(rc, "tdc_admm_project")
     return K_hat, Mn
+
+
+# ---- group norm (tdc_norm.h) and microscaled 4-bit products (tdc_mx4.h)
+
+def _check(rc: int, where: str) -> None:
+    if rc != TDC_OK:
+        raise TdcError(rc, where)
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def tdc_norm_plan_create(shape: tdc_norm_shape, device: int = 0) -> ctypes.c_void_p:
+    plan = ctypes.c_void_p()
+    _check(load().tdc_norm_plan_create(ctypes.byref(plan), ctypes.byref(shape), device), "tdc_norm_plan_create")
+    return plan
+
+
+def tdc_norm_plan_destroy(plan) -> None:
+    _check(load().tdc_norm_plan_destroy(plan), "tdc_norm_plan_destroy")
+
+
+def tdc_norm_plan_workspace_bytes(plan) -> int:
+    return int(load().tdc_norm_plan_workspace_bytes(plan))
+
+
+def tdc_norm_plan_kernel_count(plan) -> int:
+    return int(load().tdc_norm_plan_kernel_count(plan))
+
+
+def make_norm_args(residual=None, mean=None, rstd=None, x_pitch=0, residual_pitch=0, y_pitch=0) -> tdc_norm_args:
+    return tdc_norm_args(_ptr(residual), _ptr(mean), _ptr(rstd), x_pitch, residual_pitch, y_pitch)
+
+
+def tdc_group_norm(plan, x, gamma, beta, y, args: Optional[tdc_norm_args] = None, stream=None) -> None:
+    _check(load().tdc_group_norm(plan, _stream(stream), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ref(args)), "tdc_group_norm")
+
+
+def tdc_group_norm_mx4(plan, x, gamma, beta, codes, scales, args: Optional[tdc_norm_args] = None, stream=None) -> None:
+    _check(load().tdc_group_norm_mx4(plan, _stream(stream), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(codes), _ptr(scales), _ref(args)),
+           "tdc_group_norm_mx4")
+
+
+def make_norm_grad_args(residual=None, dresidual=None, x_pitch=0, residual_pitch=0, dy_pitch=0, dx_pitch=0, dresidual_pitch=0) -> tdc_norm_grad_args:
+    return tdc_norm_grad_args(_ptr(residual), _ptr(dresidual), x_pitch, residual_pitch, dy_pitch, dx_pitch, dresidual_pitch)
+
+
+def tdc_group_norm_backward(plan, x, dy, mean, rstd, gamma, beta, dx, dgamma, dbeta, args: Optional[tdc_norm_grad_args] = None, stream=None) -> None:
+    _check(load().tdc_group_norm_backward(plan, _stream(stream), _ptr(x), _ptr(dy), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(beta), _ptr(dx),
+                                          _ptr(dgamma), _ptr(dbeta), _ref(args)), "tdc_group_norm_backward")
+
+
+def tdc_mx4_quantize(x, dtype: int, rows: int, cols: int, codes, scales, pitch: int = 0, stream=None) -> None:
+    _check(load().tdc_mx4_quantize(_stream(stream), _ptr(x), dtype, rows, cols, pitch, _ptr(codes), _ptr(scales)), "tdc_mx4_quantize")
+
+
+def tdc_mx4_dequantize(codes, scales, rows: int, cols: int, y, dtype: int, pitch: int = 0, stream=None) -> None:
+    _check(load().tdc_mx4_dequantize(_stream(stream), _ptr(codes), _ptr(scales), rows, cols, _ptr(y), dtype, pitch), "tdc_mx4_dequantize")
+
+
+def make_mx4_epilogue(bias=None, residual=None, act: int = ACT_NONE) -> tdc_mx4_epilogue:
+    return tdc_mx4_epilogue(_ptr(bias), _ptr(residual), act)
+
+
+def tdc_mx4_matmul(a_codes, a_scales, b_codes, b_scales, M: int, N: int, K: int, y, dtype: int, epilogue: Optional[tdc_mx4_epilogue] = None, stream=None) -> None:
+    _check(load().tdc_mx4_matmul(_stream(stream), _ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), M, N, K, _ptr(y), dtype,
+                                 _ref(epilogue)), "tdc_mx4_matmul")
+
+
+def tdc_mx4_plan_create(shape: tdc_mx4_shape, device: int = 0) -> ctypes.c_void_p:
+    plan = ctypes.c_void_p()
+    _check(load().tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(shape), device), "tdc_mx4_plan_create")
+    return plan
+
+
+def tdc_mx4_plan_destroy(plan) -> None:
+    _check(load().tdc_mx4_plan_destroy(plan), "tdc_mx4_plan_destroy")
+
+
+def tdc_mx4_plan_workspace_bytes(plan) -> int:
+    return int(load().tdc_mx4_plan_workspace_bytes(plan))
+
+
+def tdc_mx4_plan_kernel_count(plan) -> int:
+    return int(load().tdc_mx4_plan_kernel_count(plan))
+
+
+def tdc_mx4_plan_pack(plan, W, stream=None) -> None:
+    _check(load().tdc_mx4_plan_pack(plan, _stream(stream), _ptr(W)), "tdc_mx4_plan_pack")
+
+
+def tdc_conv_mx4(plan, x, y, epilogue: Optional[tdc_mx4_epilogue] = None, stream=None) -> None:
+    _check(load().tdc_conv_mx4(plan, _stream(stream), _ptr(x), _ptr(y), _ref(epilogue)), "tdc_conv_mx4")
+
+
+def tdc_conv_mx4_quantized(plan, codes, scales, y, epilogue: Optional[tdc_mx4_epilogue] = None, stream=None) -> None:
+    _check(load().tdc_conv_mx4_quantized(plan, _stream(stream), _ptr(codes), _ptr(scales), _ptr(y), _ref(epilogue)), "tdc_conv_mx4_quantized")

@@ -29,21 +29,6 @@ namespace {
 
 __global__ void tdc_null_kernel() {}
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = (prev == dev) || (hipSetDevice(dev) == hipSuccess);
-        if (prev == dev) prev = -1;
-    }
-    ~DeviceGuard()
-    {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
-
 // NHWC kernels move x, y and the residual in 16-byte pieces
 bool misaligned16(const void *x, const void *y, const void *residual)
 {

@@ -24,6 +24,22 @@
 #include "tdc.h"
 #include "tdc_measure.h"
 
+// Makes `dev` the calling thread's device for as long as it lives.
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev)
+    {
+        if (hipGetDevice(&prev) != hipSuccess) return;
+        ok = (prev == dev) || (hipSetDevice(dev) == hipSuccess);
+        if (prev == dev) prev = -1;
+    }
+    ~DeviceGuard()
+    {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
 // Optional output epilogue, applied as the last kernel stores y:
 //   y = acc + bias[n] + residual[same element as y], then max(., 0) if relu.
 struct TdcEpi {

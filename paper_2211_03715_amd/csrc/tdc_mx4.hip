@@ -1,0 +1,272 @@
+// Microscaled 4-bit floating point: quantisation, its inverse, plans and launch dispatch (tdc_mx4.h).
+#include <initializer_list>
+#include <new>
+
+#include "tdc_mx4_internal.h"
+
+namespace {
+
+// ---- x -> codes and scales: a thread to a block
+template <typename T, int V>
+__global__ __launch_bounds__(256) void tdc_mx4_quantize_blocks(const T *__restrict__ x, TdcMx4Rows rows, int64_t total, int cols, int nb, int64_t pitch,
+                                                               uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int64_t m = i / nb;
+    const int kb = (int)(i - m * nb), c0 = kb * 32;
+    const T *p = x + rows.source(m) * pitch + c0;
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; j += V) {
+        if (c0 + j < cols) {
+            const TdcVec<T, V> in = tdc_load<T, V>(p + j);
+#pragma unroll
+            for (int u = 0; u < V; ++u) v[j + u] = (float)in.v[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < V; ++u) v[j + u] = 0.f;
+        }
+    }
+    unsigned e;
+    const tdc_i4 c = tdc_mx4_block(v, e);
+    *reinterpret_cast<tdc_i4 *>(codes + i * 16) = c;
+    scales[i] = (uint8_t)e;
+}
+
+// ---- W[C][N] -> codes and scales of [N][C]: a thread to a block, neighbours along N
+__global__ __launch_bounds__(256) void tdc_mx4_pack_weights(const float *__restrict__ W, int C, int N, int nb, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    for (int kb = blockIdx.y; kb < nb; kb += gridDim.y) {
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = 32 * kb + j < C ? W[(size_t)(32 * kb + j) * N + n] : 0.f;
+        unsigned e;
+        const tdc_i4 c = tdc_mx4_block(v, e);
+        *reinterpret_cast<tdc_i4 *>(codes + ((size_t)n * nb + kb) * 16) = c;
+        scales[(size_t)n * nb + kb] = (uint8_t)e;
+    }
+}
+
+// ---- codes and scales -> values, a thread to eight of them
+template <typename T, int V>
+__global__ __launch_bounds__(256) void tdc_mx4_dequantize_values(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t total, int cols, int nb,
+                                                                 int64_t pitch, T *__restrict__ y)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int64_t block = i >> 2, m = block / nb;
+    const int c0 = (int)(block - m * nb) * 32 + (int)(i & 3) * 8;
+    if (c0 >= cols) return;
+    const unsigned c = reinterpret_cast<const unsigned *>(codes)[i];
+    float v[8];
+    tdc_mx4_values8(c, scales[block], v);
+    T *out = y + m * pitch + c0;
+#pragma unroll
+    for (int j = 0; j < 8; j += V) {
+        if (c0 + j < cols) {
+            float o[V];
+#pragma unroll
+            for (int u = 0; u < V; ++u) o[u] = v[j + u];
+            tdc_store<T, V>(out + j, o);
+        }
+    }
+}
+
+// The most neighbours that one access of rows of `cols` may take.
+int row_vec(int dtype, int64_t cols, int64_t pitch, const void *p)
+{
+    const int size = tdc_dtype_bytes(dtype);
+    for (int v = 16 / size; v > 1; v /= 2)
+        if (cols % v == 0 && pitch % v == 0 && tdc_aligned_to(p, (size_t)v * size)) return v;
+    return 1;
+}
+
+// Workgroups of a launch along x; 0 where there are too many.
+unsigned blocks_for(int64_t items, int64_t per_block)
+{
+    const int64_t n = (items + per_block - 1) / per_block;
+    return n > 0x7fffffff / 256 ? 0u : (unsigned)n;
+}
+
+hipError_t launch_quantize(hipStream_t s, const void *x, int dtype, const TdcMx4Rows &rows, int64_t n_rows, int cols, int64_t pitch, uint8_t *codes, uint8_t *scales)
+{
+    const int nb = tdc_mx4_blocks(cols);
+    const int64_t total = n_rows * nb;
+    const unsigned grid = blocks_for(total, 256);
+    if (!grid) return hipErrorInvalidValue;
+    TDC_FOR_DTYPE(dtype, T, TDC_FOR_VEC(row_vec(dtype, cols, pitch, x), T, V, {
+        tdc_mx4_quantize_blocks<T, V><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, nb, pitch, codes, scales);
+    }));
+    return hipGetLastError();
+}
+
+int check_epilogue(const tdc_mx4_epilogue *e, int dtype)
+{
+    if (!e) return TDC_OK;
+    if (!tdc_known_act(e->act)) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_aligned_to(e->bias, 4) || !tdc_aligned_to(e->residual, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    return TDC_OK;
+}
+
+TdcMx4Epi kernel_epilogue(const tdc_mx4_epilogue *e)
+{
+    return e ? TdcMx4Epi{e->bias, e->residual, e->act} : TdcMx4Epi{nullptr, nullptr, TDC_ACT_NONE};
+}
+
+}  // namespace
+
+struct tdc_mx4_plan {
+    tdc_mx4_shape shape;
+    int device;
+    int64_t rows;            // output pixels
+    TdcMx4Rows map;          // output pixel -> input pixel
+    uint8_t *w_codes, *w_scales, *x_codes, *x_scales;
+    bool packed;
+    size_t ws_bytes;
+};
+
+extern "C" {
+
+int tdc_mx4_quantize(void *hip_stream, const void *x, int dtype, int64_t rows, int64_t cols, int64_t pitch, uint8_t *codes, uint8_t *scales)
+{
+    if (rows == 0 && cols > 0) return tdc_known_dtype(dtype) ? TDC_OK : TDC_ERR_UNSUPPORTED;
+    if (!x || !codes || !scales) return TDC_ERR_NULL;
+    if (pitch == 0) pitch = cols;
+    if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
+    if (!tdc_known_dtype(dtype) || cols > 0x7fffffff - 31 || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(x, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (rows > INT64_MAX / 64 / tdc_mx4_blocks((int)cols) || !blocks_for(rows * tdc_mx4_blocks((int)cols), 256)) return TDC_ERR_UNSUPPORTED;
+    return launch_quantize((hipStream_t)hip_stream, x, dtype, TdcMx4Rows::all(), rows, (int)cols, pitch, codes, scales) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+int tdc_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *y, int dtype, int64_t pitch)
+{
+    if (rows == 0 && cols > 0) return tdc_known_dtype(dtype) ? TDC_OK : TDC_ERR_UNSUPPORTED;
+    if (!y || !codes || !scales) return TDC_ERR_NULL;
+    if (pitch == 0) pitch = cols;
+    if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
+    if (!tdc_known_dtype(dtype) || cols > 0x7fffffff - 31 || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    const int nb = tdc_mx4_blocks((int)cols);
+    if (rows > INT64_MAX / 64 / nb) return TDC_ERR_UNSUPPORTED;
+    const int64_t total = rows * nb * 4;
+    const unsigned grid = blocks_for(total, 256);
+    if (!grid) return TDC_ERR_UNSUPPORTED;
+    hipStream_t s = (hipStream_t)hip_stream;
+    TDC_FOR_DTYPE(dtype, T, TDC_FOR_VEC(row_vec(dtype, cols, pitch, y), T, V, {
+        tdc_mx4_dequantize_values<T, V><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, nb, pitch, (T *)y);
+    }));
+    return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes, const uint8_t *b_scales, int32_t M, int32_t N, int32_t K,
+                   void *y, int dtype, const tdc_mx4_epilogue *epilogue)
+{
+    if (M < 0 || N < 1 || K < 1) return TDC_ERR_BAD_SHAPE;
+    if (!tdc_known_dtype(dtype)) return TDC_ERR_UNSUPPORTED;
+    if (M == 0) return check_epilogue(epilogue, dtype);
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !y) return TDC_ERR_NULL;
+    const int rc = check_epilogue(epilogue, dtype);
+    if (rc != TDC_OK) return rc;
+    if (K > 0x7fffffff - 31 || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_mx4_product_fits(M, N)) return TDC_ERR_UNSUPPORTED;
+    const TdcMx4Product q{a_codes, a_scales, b_codes, b_scales, M, N, tdc_mx4_blocks(K), TdcMx4Rows::all(), y, kernel_epilogue(epilogue)};
+    return tdc_launch_mx4_product(q, dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int device)
+{
+    if (!out || !shape) return TDC_ERR_NULL;
+    *out = nullptr;
+    tdc_mx4_shape s = *shape;
+    if (s.batch < 1 || s.H < 1 || s.W < 1 || s.C < 1 || s.N < 1 || s.stride < 1) return TDC_ERR_BAD_SHAPE;
+    if (s.x_pitch == 0) s.x_pitch = s.C;
+    if (s.x_pitch < s.C) return TDC_ERR_BAD_SHAPE;
+    const int64_t Ho = (s.H - 1) / s.stride + 1, Wo = (s.W - 1) / s.stride + 1, lim = 0x7fffffff;
+    if (!tdc_known_dtype(s.dtype) || s.C > lim - 31) return TDC_ERR_UNSUPPORTED;
+    if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
+    const int64_t rows = s.batch * Ho * Wo;
+    if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 256)) return TDC_ERR_UNSUPPORTED;
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev) return TDC_ERR_HIP;
+    DeviceGuard guard(device);
+    if (!guard.ok) return TDC_ERR_HIP;
+    tdc_mx4_plan *p = new (std::nothrow) tdc_mx4_plan();
+    if (!p) return TDC_ERR_ALLOC;
+    p->shape = s;
+    p->device = device;
+    p->rows = rows;
+    p->map = s.stride == 1 ? TdcMx4Rows::all() : TdcMx4Rows{s.stride, (int)Wo, (int)(Ho * Wo), s.W, s.H * s.W};
+    const size_t nb = tdc_mx4_blocks(s.C);
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t parts[4] = {up(s.N * nb * 16), up(s.N * nb), up(rows * nb * 16), up(rows * nb)};
+    p->ws_bytes = parts[0] + parts[1] + parts[2] + parts[3];
+    if (hipMalloc((void **)&p->w_codes, p->ws_bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        delete p;
+        return TDC_ERR_ALLOC;
+    }
+    p->w_scales = p->w_codes + parts[0];
+    p->x_codes = p->w_scales + parts[1];
+    p->x_scales = p->x_codes + parts[2];
+    *out = p;
+    return TDC_OK;
+}
+
+int tdc_mx4_plan_destroy(tdc_mx4_plan *p)
+{
+    if (!p) return TDC_OK;
+    DeviceGuard guard(p->device);
+    const int rc = hipFree(p->w_codes) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    delete p;
+    return rc;
+}
+
+size_t tdc_mx4_plan_workspace_bytes(const tdc_mx4_plan *p) { return p ? p->ws_bytes : 0; }
+
+int tdc_mx4_plan_kernel_count(const tdc_mx4_plan *p) { return p ? 2 : 0; }
+
+int tdc_mx4_plan_pack(tdc_mx4_plan *p, void *hip_stream, const float *W)
+{
+    if (!p || !W) return TDC_ERR_NULL;
+    if (!tdc_aligned_to(W, 4)) return TDC_ERR_UNSUPPORTED;
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return TDC_ERR_HIP;
+    const int C = p->shape.C, N = p->shape.N, nb = tdc_mx4_blocks(C);
+    const dim3 grid((N + 255) / 256, nb < 65535 ? nb : 65535);
+    tdc_mx4_pack_weights<<<grid, 256, 0, (hipStream_t)hip_stream>>>(W, C, N, nb, p->w_codes, p->w_scales);
+    if (hipGetLastError() != hipSuccess) return TDC_ERR_HIP;
+    p->packed = true;
+    return TDC_OK;
+}
+
+int tdc_conv_mx4(tdc_mx4_plan *p, void *hip_stream, const void *x, void *y, const tdc_mx4_epilogue *epilogue)
+{
+    if (!p || !p->packed || !x || !y) return TDC_ERR_NULL;
+    const tdc_mx4_shape &s = p->shape;
+    const int rc = check_epilogue(epilogue, s.dtype);
+    if (rc != TDC_OK) return rc;
+    if (!tdc_aligned_to(x, tdc_dtype_bytes(s.dtype)) || !tdc_aligned_to(y, tdc_dtype_bytes(s.dtype))) return TDC_ERR_UNSUPPORTED;
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return TDC_ERR_HIP;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (launch_quantize(st, x, s.dtype, p->map, p->rows, s.C, s.x_pitch, p->x_codes, p->x_scales) != hipSuccess) return TDC_ERR_HIP;
+    const TdcMx4Product q{p->x_codes, p->x_scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), TdcMx4Rows::all(), y, kernel_epilogue(epilogue)};
+    return tdc_launch_mx4_product(q, s.dtype, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+int tdc_conv_mx4_quantized(tdc_mx4_plan *p, void *hip_stream, const uint8_t *codes, const uint8_t *scales, void *y, const tdc_mx4_epilogue *epilogue)
+{
+    if (!p || !p->packed || !codes || !scales || !y) return TDC_ERR_NULL;
+    const tdc_mx4_shape &s = p->shape;
+    const int rc = check_epilogue(epilogue, s.dtype);
+    if (rc != TDC_OK) return rc;
+    if (!tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(s.dtype))) return TDC_ERR_UNSUPPORTED;
+    DeviceGuard guard(p->device);
+    if (!guard.ok) return TDC_ERR_HIP;
+    const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue)};
+    return tdc_launch_mx4_product(q, s.dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+}  // extern "C"

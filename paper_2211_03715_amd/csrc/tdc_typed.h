@@ -1,0 +1,88 @@
+// Elements of the three activation types and what kernels do with them: loads and stores of V neighbours at once, sums over
+// lanes, activations.  Shared by the norm and the 4-bit kernels.
+#ifndef TDC_TYPED_H
+#define TDC_TYPED_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tdc_internal.h"
+#include "tdc_norm.h"
+
+typedef _Float16 tdc_half;
+typedef __bf16 tdc_bf16;
+
+inline int tdc_dtype_bytes(int dtype) { return dtype == TDC_F32 ? 4 : 2; }
+inline bool tdc_known_dtype(int dtype) { return dtype == TDC_F32 || dtype == TDC_F16 || dtype == TDC_BF16; }
+inline bool tdc_known_act(int act) { return act == TDC_ACT_NONE || act == TDC_ACT_RELU || act == TDC_ACT_SILU; }
+inline bool tdc_aligned_to(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// V neighbours, V * sizeof(T) <= 16 a power of two: one load.  The pointer is aligned to all of them.
+template <typename T, int V> struct __align__(sizeof(T) * V) TdcVec {
+    T v[V];
+};
+
+template <typename T, int V> __device__ __forceinline__ TdcVec<T, V> tdc_load(const T *p)
+{
+    return *reinterpret_cast<const TdcVec<T, V> *>(p);
+}
+
+template <typename T, int V> __device__ __forceinline__ void tdc_store(T *p, const float (&f)[V])
+{
+    TdcVec<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = (T)f[i];
+    *reinterpret_cast<TdcVec<T, V> *>(p) = o;
+}
+
+// 1 / (1 + exp(-v)): v_exp and v_rcp are good to about an ulp each, and both ends are right: exp(-v) = inf gives 0, 0 gives 1.
+__device__ __forceinline__ float tdc_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+template <int ACT> __device__ __forceinline__ float tdc_activate(float v)
+{
+    if constexpr (ACT == TDC_ACT_RELU) return v > 0.f ? v : (v != v ? v : 0.f);   // a NaN stays one
+    if constexpr (ACT == TDC_ACT_SILU) return v * tdc_sigmoid(v);
+    return v;
+}
+
+// act'(v)
+template <int ACT> __device__ __forceinline__ float tdc_activate_grad(float v)
+{
+    if constexpr (ACT == TDC_ACT_RELU) return v > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == TDC_ACT_SILU) {
+        const float s = tdc_sigmoid(v);
+        return s * (1.f + v * (1.f - s));
+    }
+    return 1.f;
+}
+
+// Sum over the neighbouring `lanes` lanes (a power of two up to 64), the same in each of them.
+__device__ __forceinline__ float tdc_lane_sum(float v, int lanes)
+{
+    for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// The statements for a dtype with T its type, for an activation with the constant ACT, for V neighbours with the constant V.
+#define TDC_FOR_DTYPE(dtype, T, ...)                                  \
+    do {                                                              \
+        if ((dtype) == TDC_F32) { using T = float; __VA_ARGS__; }     \
+        else if ((dtype) == TDC_F16) { using T = tdc_half; __VA_ARGS__; } \
+        else { using T = tdc_bf16; __VA_ARGS__; }                     \
+    } while (0)
+#define TDC_FOR_ACT(act, ACT, ...)                                                              \
+    do {                                                                                        \
+        if ((act) == TDC_ACT_RELU) { constexpr int ACT = TDC_ACT_RELU; __VA_ARGS__; }           \
+        else if ((act) == TDC_ACT_SILU) { constexpr int ACT = TDC_ACT_SILU; __VA_ARGS__; }      \
+        else { constexpr int ACT = TDC_ACT_NONE; __VA_ARGS__; }                                 \
+    } while (0)
+
+#define TDC_FOR_VEC(v, T, V, ...)                                                         \
+    do {                                                                                  \
+        if ((v) == 8) { if constexpr (sizeof(T) == 2) { constexpr int V = 8; __VA_ARGS__; } } \
+        else if ((v) == 4) { constexpr int V = 4; __VA_ARGS__; }                          \
+        else if ((v) == 2) { constexpr int V = 2; __VA_ARGS__; }                          \
+        else { constexpr int V = 1; __VA_ARGS__; }                                        \
+    } while (0)
+
+#endif  // TDC_TYPED_H

@@ -1,0 +1,117 @@
+"""Group norm and 4-bit products without a GPU: refusals come before any device call, struct layouts match the headers, and the
+64-bit references agree with hand-worked values and with differences."""
+import ctypes
+
+import pytest
+import torch
+
+import mx4_reference as R
+from paper_2211_03715_amd import binding as B
+
+P = ctypes.c_void_p(4096)          # an address that is never read
+ODD = ctypes.c_void_p(4097)
+
+
+def test_struct_layouts():
+    assert ctypes.sizeof(B.tdc_norm_shape) == 32 and ctypes.sizeof(B.tdc_norm_args) == 48 and ctypes.sizeof(B.tdc_norm_grad_args) == 56
+    assert ctypes.sizeof(B.tdc_mx4_shape) == 40 and ctypes.sizeof(B.tdc_mx4_epilogue) == 24
+
+
+def _norm(**kw):
+    d = dict(batch=1, H=2, W=2, C=8, groups=2, dtype=0, act=0, eps=1e-5)
+    d.update(kw)
+    return B.tdc_norm_shape(*(d[k] for k in ("batch", "H", "W", "C", "groups", "dtype", "act", "eps")))
+
+
+def test_norm_plans_are_refused():
+    lib, plan = B.load(), ctypes.c_void_p()
+    make = lambda **kw: lib.tdc_norm_plan_create(ctypes.byref(plan), ctypes.byref(_norm(**kw)), 0)
+    assert lib.tdc_norm_plan_create(None, ctypes.byref(_norm()), 0) == B.TDC_ERR_NULL
+    assert lib.tdc_norm_plan_create(ctypes.byref(plan), None, 0) == B.TDC_ERR_NULL
+    for bad in (dict(batch=0), dict(H=0), dict(W=-1), dict(C=0), dict(groups=0), dict(groups=3), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf"))):
+        assert make(**bad) == B.TDC_ERR_BAD_SHAPE and not plan.value, bad
+    for bad in (dict(dtype=3), dict(dtype=-1), dict(act=3), dict(batch=65536), dict(C=16384), dict(H=65536, W=65536)):
+        assert make(**bad) == B.TDC_ERR_UNSUPPORTED and not plan.value, bad
+    assert lib.tdc_norm_plan_destroy(None) == B.TDC_OK and lib.tdc_norm_plan_workspace_bytes(None) == 0 and lib.tdc_norm_plan_kernel_count(None) == 0
+    assert lib.tdc_group_norm(None, None, P, None, None, P, None) == B.TDC_ERR_NULL
+    assert lib.tdc_group_norm_mx4(None, None, P, None, None, P, P, None) == B.TDC_ERR_NULL
+    assert lib.tdc_group_norm_backward(None, None, P, P, P, P, None, None, P, P, P, None) == B.TDC_ERR_NULL
+
+
+def test_quantisation_is_refused():
+    q, d = B.load().tdc_mx4_quantize, B.load().tdc_mx4_dequantize
+    assert q(None, P, 0, 0, 8, 0, P, P) == B.TDC_OK and d(None, P, P, 0, 8, P, 0, 0) == B.TDC_OK        # no rows, nothing to do
+    for call in (lambda p, t, r, c, s, k: q(None, p, t, r, c, s, k, P), lambda p, t, r, c, s, k: d(None, k, P, r, c, p, t, s)):
+        assert call(None, 0, 1, 8, 0, P) == B.TDC_ERR_NULL and call(P, 0, 1, 8, 0, None) == B.TDC_ERR_NULL
+        assert call(P, 0, -1, 8, 0, P) == B.TDC_ERR_BAD_SHAPE and call(P, 0, 1, 0, 0, P) == B.TDC_ERR_BAD_SHAPE and call(P, 0, 1, 8, 7, P) == B.TDC_ERR_BAD_SHAPE
+        assert call(P, 3, 1, 8, 0, P) == B.TDC_ERR_UNSUPPORTED and call(P, 3, 0, 8, 0, P) == B.TDC_ERR_UNSUPPORTED
+        assert call(ODD, 1, 1, 8, 0, P) == B.TDC_ERR_UNSUPPORTED and call(P, 0, 1, 8, 0, ctypes.c_void_p(4104)) == B.TDC_ERR_UNSUPPORTED
+        assert call(P, 0, 1, 1 << 31, 0, P) == B.TDC_ERR_UNSUPPORTED and call(P, 0, 1 << 40, 8, 0, P) == B.TDC_ERR_UNSUPPORTED
+        assert call(P, 0, 1 << 62, 1 << 30, 0, P) == B.TDC_ERR_UNSUPPORTED
+
+
+def test_products_are_refused():
+    fn = B.load().tdc_mx4_matmul
+    call = lambda a=P, sa=P, b=P, sb=P, M=4, N=4, K=32, y=P, t=0, e=None: fn(None, a, sa, b, sb, M, N, K, y, t, ctypes.byref(e) if e is not None else None)
+    assert call(M=0) == B.TDC_OK
+    for bad in (dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(y=None)):
+        assert call(**bad) == B.TDC_ERR_NULL, bad
+    for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(K=-5)):
+        assert call(**bad) == B.TDC_ERR_BAD_SHAPE, bad
+    for bad in (dict(t=3), dict(a=ctypes.c_void_p(4104)), dict(b=ODD), dict(y=ODD), dict(M=1 << 30, N=1 << 20), dict(K=0x7fffffff),
+                dict(e=B.make_mx4_epilogue(act=3)), dict(e=B.make_mx4_epilogue(bias=4098)), dict(e=B.make_mx4_epilogue(residual=4098))):
+        assert call(**bad) == B.TDC_ERR_UNSUPPORTED, bad
+
+
+def _mx4(**kw):
+    d = dict(batch=1, H=2, W=2, C=8, N=4, stride=1, dtype=0, x_pitch=0)
+    d.update(kw)
+    return B.tdc_mx4_shape(*(d[k] for k in ("batch", "H", "W", "C", "N", "stride", "dtype", "x_pitch")))
+
+
+def test_convolution_plans_are_refused():
+    lib, plan = B.load(), ctypes.c_void_p()
+    make = lambda **kw: lib.tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(_mx4(**kw)), 0)
+    assert lib.tdc_mx4_plan_create(None, ctypes.byref(_mx4()), 0) == B.TDC_ERR_NULL and lib.tdc_mx4_plan_create(ctypes.byref(plan), None, 0) == B.TDC_ERR_NULL
+    for bad in (dict(batch=0), dict(H=0), dict(W=0), dict(C=0), dict(N=0), dict(stride=0), dict(x_pitch=7), dict(x_pitch=-8)):
+        assert make(**bad) == B.TDC_ERR_BAD_SHAPE and not plan.value, bad
+    for bad in (dict(dtype=3), dict(C=0x7fffffff), dict(batch=65536, H=256, W=256), dict(batch=1 << 20, H=32, W=32, N=1 << 20)):
+        assert make(**bad) == B.TDC_ERR_UNSUPPORTED and not plan.value, bad
+    assert lib.tdc_mx4_plan_destroy(None) == B.TDC_OK and lib.tdc_mx4_plan_workspace_bytes(None) == 0 and lib.tdc_mx4_plan_kernel_count(None) == 0
+    assert lib.tdc_mx4_plan_pack(None, None, P) == B.TDC_ERR_NULL and lib.tdc_conv_mx4(None, None, P, P, None) == B.TDC_ERR_NULL
+    assert lib.tdc_conv_mx4_quantized(None, None, P, P, P, None) == B.TDC_ERR_NULL
+
+
+def test_python_layers_refuse_what_is_not_on_a_gpu():
+    from paper_2211_03715_amd import mx4
+    with pytest.raises(ValueError):
+        mx4.quantize(torch.zeros(2, 32))
+    with pytest.raises(ValueError):
+        mx4.quantize(torch.zeros(2, 32, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        mx4.dequantize(torch.zeros(2, 16, dtype=torch.uint8), torch.zeros(2, 1, dtype=torch.uint8), 32)
+    from paper_2211_03715_amd.workloads import Layer
+    with pytest.raises(ValueError):
+        mx4.MX4Conv2d(Layer(1, 8, 8, 4, 4, 1, 1))
+
+
+def test_reference_quantisation_by_hand():
+    x = torch.zeros(2, 34, dtype=torch.float64)
+    # largest 6: scale 1.  Ties at 1/4, 3/4, 5/4, 7/4, 5/2, 7/2, 5 go to 0, 1, 1, 2, 2, 4, 4.
+    x[0, :9] = torch.tensor([6, .25, .75, -1.25, 1.75, 2.5, 3.5, 5, -.2])
+    x[0, 32:] = torch.tensor([7.9, 1.0])              # largest in [4, 8): scale 1, 7.9 becomes 6
+    x[1, 0] = float("inf")
+    x[1, 33] = 2.0 ** -149                            # 2^(-149-2) is below the least scale, 2^-127
+    codes, scales = R.quantize(x)
+    assert scales.tolist() == [[127, 127], [255, 0]]
+    v = R.values(codes, scales, 34)
+    assert v[0, :9].tolist() == [6, 0, 1, -1, 2, 2, 4, 4, -0.0] and v[0, 32:].tolist() == [6, 1]
+    assert bool(torch.isnan(v[1, :32]).all()) and v[1, 32:].tolist() == [0, 0]
+    assert codes[0, :2].tolist() == [7, 2 + 16 * (8 + 2)]
+
+
+def test_reference_norm_by_hand():
+    x = torch.tensor([1., 3, 10, 10, 5, 7, 10, 14]).reshape(1, 1, 2, 4)      # groups of two channels: {1, 3, 5, 7}, {10, 10, 10, 14}
+    pre, xhat, mean, rstd = R.group_norm(x, 2, 0.0)
+    assert mean.tolist() == [[4, 11]] and torch.allclose(rstd, torch.tensor([[5.0 ** -.5, 3.0 ** -.5]], dtype=torch.float64))
+    assert torch.allclose(xhat[0, 0, 0], torch.tensor([-3, -1, 0, 0], dtype=torch.float64) * rstd[0].repeat_interleave(2) + torch.tensor([0, 0, -1, -1]) * rstd[0, 1])
