@@ -171,7 +171,7 @@ int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_sc
     if (rc != TDC_OK) return rc;
     if (K > 0x7fffffff - 31 || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     if (!tdc_mx4_product_fits(M, N)) return TDC_ERR_UNSUPPORTED;
-    const TdcMx4Product q{a_codes, a_scales, b_codes, b_scales, M, N, tdc_mx4_blocks(K), TdcMx4Rows::all(), y, kernel_epilogue(epilogue)};
+    const TdcMx4Product q{a_codes, a_scales, b_codes, b_scales, M, N, tdc_mx4_blocks(K), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
@@ -252,7 +252,7 @@ int tdc_conv_mx4(tdc_mx4_plan *p, void *hip_stream, const void *x, void *y, cons
     if (!guard.ok) return TDC_ERR_HIP;
     hipStream_t st = (hipStream_t)hip_stream;
     if (launch_quantize(st, x, s.dtype, p->map, p->rows, s.C, s.x_pitch, p->x_codes, p->x_scales) != hipSuccess) return TDC_ERR_HIP;
-    const TdcMx4Product q{p->x_codes, p->x_scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), TdcMx4Rows::all(), y, kernel_epilogue(epilogue)};
+    const TdcMx4Product q{p->x_codes, p->x_scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, s.dtype, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
@@ -265,7 +265,7 @@ int tdc_conv_mx4_quantized(tdc_mx4_plan *p, void *hip_stream, const uint8_t *cod
     if (!tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(s.dtype))) return TDC_ERR_UNSUPPORTED;
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
-    const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue)};
+    const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, s.dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 

@@ -34,6 +34,7 @@ struct TdcMx4Product {
     TdcMx4Rows a_rows;
     void *y;
     TdcMx4Epi epi;
+    bool vec;                // y and the residual can be accessed 16 bytes at a time
 };
 
 // Whether the kernels' grids cover M x N outputs.

@@ -3,28 +3,9 @@
 // v_mfma_scale_f32_32x32x64: lane l holds the 32 values of row l%32 that one block of k holds (block l/32 of the two), 16
 // bytes, with the block's scale beside it, so an operand in the format's own layout needs no rearrangement.  Of the result,
 // register i of lane l is element [m = 8*(i/4) + 4*(l/32) + i%4][n = l%32] with rows of A as m and rows of B as n.
-#include "tdc_mx4_internal.h"
+#include "tdc_mx4_tile.h"
 
 namespace {
-
-typedef float f16v __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ tdc_i8 widen(tdc_i4 a) { return __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1); }
-
-__device__ __forceinline__ f16v mfma(tdc_i4 a, unsigned sa, tdc_i4 b, unsigned sb, f16v c)
-{
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(a), widen(b), c, 4, 4, 0, (int)sa, 0, (int)sb);
-}
-
-template <typename T> __device__ __forceinline__ void finish(const TdcMx4Product &q, float v, int m, int n)
-{
-    const size_t at = (size_t)m * q.N + n;
-    if (q.epi.bias) v += q.epi.bias[n];
-    if (q.epi.residual) v += (float)static_cast<const T *>(q.epi.residual)[at];
-    if (q.epi.act == TDC_ACT_RELU) v = tdc_activate<TDC_ACT_RELU>(v);
-    else if (q.epi.act == TDC_ACT_SILU) v = tdc_activate<TDC_ACT_SILU>(v);
-    static_cast<T *>(q.y)[at] = (T)v;
-}
 
 // A wavefront to 32 x 32 outputs, operands straight from memory.
 template <typename T>
@@ -36,7 +17,7 @@ __global__ __launch_bounds__(256) void tdc_mx4_product_simple(TdcMx4Product q)
     const int m0 = (int)(tile / nblocks) * 32, n0 = (int)(tile % nblocks) * 32;
     // rows past the end read the last one: what they give is not stored
     const size_t ra = (size_t)q.a_rows.source(min(m0 + (l & 31), q.M - 1)) * q.nb, rb = (size_t)min(n0 + (l & 31), q.N - 1) * q.nb;
-    f16v acc;
+    tdc_f16v acc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
     for (int k = 0; k < q.nb; k += 2) {
@@ -49,20 +30,29 @@ __global__ __launch_bounds__(256) void tdc_mx4_product_simple(TdcMx4Product q)
             sa = q.a_scales[ra + kb];
             sb = q.b_scales[rb + kb];
         }
-        acc = mfma(a, sa, b, sb, acc);
+        acc = tdc_mx4_mfma<0>(a, sa, b, sb, acc);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int m = m0 + 8 * (i / 4) + 4 * (l >> 5) + i % 4, n = n0 + (l & 31);
-        if (m < q.M && n < q.N) finish<T>(q, acc[i], m, n);
+        float v[1] = {acc[i]};
+        if (m < q.M && n < q.N) tdc_mx4_finish<T, 1>(q, v, m, n);
     }
 }
 
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 }  // namespace
 
-hipError_t tdc_launch_mx4_product(const TdcMx4Product &q, int dtype, hipStream_t s)
+hipError_t tdc_launch_mx4_product(const TdcMx4Product &given, int dtype, hipStream_t s)
 {
-    const int64_t tiles = (int64_t)((q.M + 31) / 32) * ((q.N + 31) / 32);
-    TDC_FOR_DTYPE(dtype, T, { tdc_mx4_product_simple<T><<<(unsigned)((tiles + 3) / 4), 256, 0, s>>>(q); });
+    TdcMx4Product q = given;
+    q.vec = q.N % (16 / tdc_dtype_bytes(dtype)) == 0 && tdc_aligned_to(q.y, 16) && tdc_aligned_to(q.epi.residual, 16);
+    const int64_t large = up(q.M, 256) * up(q.N, 256), small = up(q.M, 128) * up(q.N, 128), tiles = up(q.M, 32) * up(q.N, 32);
+    TDC_FOR_DTYPE(dtype, T, {
+        if (large >= 128) tdc_mx4_product_tile<T, 4, 4><<<(unsigned)large, 256, 0, s>>>(q);
+        else if (small >= 64) tdc_mx4_product_tile<T, 2, 2><<<(unsigned)small, 256, 0, s>>>(q);
+        else tdc_mx4_product_simple<T><<<(unsigned)((tiles + 3) / 4), 256, 0, s>>>(q);
+    });
     return hipGetLastError();
 }
