@@ -100,10 +100,10 @@ __device__ __forceinline__ void tdc_mx4_tile_at(int id, int mt, int nt, int &m, 
     n = r / rows;
 }
 
-template <typename T, int WM, int WN>
-__global__ __launch_bounds__(256, WM == 4 ? 1 : 2) void tdc_mx4_product_tile(TdcMx4Product q)
+template <typename T, int WM, int WN, int GM, int GN>
+__global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Product q)
 {
-    constexpr int BM = 64 * WM, BN = 64 * WN;
+    constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, THREADS = 64 * GM * GN;
     __shared__ __attribute__((aligned(128))) uint8_t codes[2][(BM + BN) * 128];
     __shared__ uint2 scales[2][BM + BN];
     const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
@@ -112,16 +112,16 @@ __global__ __launch_bounds__(256, WM == 4 ? 1 : 2) void tdc_mx4_product_tile(Tdc
     const int m0 = tm * BM, n0 = tn * BN;
 
     // fetch: rows tid/8 + 32 i of both operands, block tid%8 of the eight; scales of rows tid + 256 i
-    constexpr int FA = BM / 32, FB = BN / 32, SR = (BM + BN) / 256;
+    constexpr int STEP = THREADS / 8, FA = BM / STEP, FB = BN / STEP, SR = (BM + BN + THREADS - 1) / THREADS;
     const int fr = tid >> 3, fk = tid & 7;
     const uint8_t *src[FA + FB], *ssrc[SR];
 #pragma unroll
-    for (int i = 0; i < FA; ++i) src[i] = q.a_codes + (size_t)q.a_rows.source(min(m0 + fr + 32 * i, q.M - 1)) * q.nb * 16;
+    for (int i = 0; i < FA; ++i) src[i] = q.a_codes + (size_t)q.a_rows.source(min(m0 + fr + STEP * i, q.M - 1)) * q.nb * 16;
 #pragma unroll
-    for (int i = 0; i < FB; ++i) src[FA + i] = q.b_codes + (size_t)min(n0 + fr + 32 * i, q.N - 1) * q.nb * 16;
+    for (int i = 0; i < FB; ++i) src[FA + i] = q.b_codes + (size_t)min(n0 + fr + STEP * i, q.N - 1) * q.nb * 16;
 #pragma unroll
     for (int i = 0; i < SR; ++i) {
-        const int r = tid + 256 * i;
+        const int r = tid + THREADS * i;
         ssrc[i] = r < BM ? q.a_scales + (size_t)q.a_rows.source(min(m0 + r, q.M - 1)) * q.nb : q.b_scales + (size_t)min(n0 + r - BM, q.N - 1) * q.nb;
     }
     tdc_i4 in[FA + FB];
@@ -133,15 +133,15 @@ __global__ __launch_bounds__(256, WM == 4 ? 1 : 2) void tdc_mx4_product_tile(Tdc
 #pragma unroll
         for (int i = 0; i < SR; ++i) sin[i] = tdc_mx4_scales8(ssrc[i], k, q.nb);
     };
-    const int wslot = fr * 128 + ((fk ^ (fr & 7)) << 4);
+    const int wslot = fr * 128 + ((fk ^ ((fr >> 1) & 7)) << 4);
     auto put = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < FA + FB; ++i) *reinterpret_cast<tdc_i4 *>(&codes[buf][wslot + i * 32 * 128]) = in[i];
+        for (int i = 0; i < FA + FB; ++i) *reinterpret_cast<tdc_i4 *>(&codes[buf][wslot + i * STEP * 128]) = in[i];
 #pragma unroll
-        for (int i = 0; i < SR; ++i) scales[buf][tid + 256 * i] = sin[i];
+        for (int i = 0; i < SR; ++i) scales[buf][tid + THREADS * i] = sin[i];
     };
 
-    const int r32 = l & 31, h = l >> 5, wm = (wave >> 1) * 32 * WM, wn = (wave & 1) * 32 * WN;
+    const int r32 = l & 31, h = l >> 5, wm = (wave / GN) * 32 * WM, wn = (wave % GN) * 32 * WN;
     tdc_f16v acc[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256, WM == 4 ? 1 : 2) void tdc_mx4_product_tile(Tdc
         const uint8_t *pa = &codes[buf][(wm + r32) * 128], *pb = &codes[buf][(BM + wn + r32) * 128];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int at = ((2 * s + h) ^ (r32 & 7)) << 4;
+            const int at = ((2 * s + h) ^ ((r32 >> 1) & 7)) << 4;
             tdc_i4 a[WM], b[WN];
 #pragma unroll
             for (int i = 0; i < WM; ++i) a[i] = *reinterpret_cast<const tdc_i4 *>(pa + i * 32 * 128 + at);
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256, WM == 4 ? 1 : 2) void tdc_mx4_product_tile(Tdc
     // 32 rows at a time through a piece of LDS of the wavefront's own, so that stores are rows of whole lines.  A pitch of 8 more
     // than a multiple of 32 keeps the two halves of a wavefront, four rows apart, on different banks.
     constexpr int COLS = 32 * WN, PITCH = COLS + 8;
-    static_assert(4 * 32 * PITCH * sizeof(float) <= sizeof(codes), "the sums fit where the codes were");
+    static_assert(GM * GN * 32 * PITCH * sizeof(float) <= sizeof(codes), "the sums fit where the codes were");
     float *sums = reinterpret_cast<float *>(&codes[0][0]) + wave * 32 * PITCH;
     __syncthreads();
 #pragma unroll
