@@ -3,8 +3,8 @@
 // Four wavefronts, two by two, share a tile of 64 WM x 64 WN outputs; each computes WM x WN blocks of 32 x 32.  A step takes 256
 // values of k, 128 bytes of codes to a row: a wavefront's fetch covers eight rows of one cache line each.  In LDS a row keeps
 // its 128 bytes, its eight blocks of 16 bytes in the order (block ^ row % 8), so that the eight rows that one pass of a 16-byte
-// read covers fall on different banks.  The next step's codes and scales travel through registers while this step multiplies,
-// and go to the other of two buffers: one barrier to a step.
+// read covers fall on different banks.  The next step's codes go straight to the other of two buffers while this step
+// multiplies, its scales through a register: one barrier to a step.
 //
 // Per matrix instruction (32 cycles for 64 kFLOP) a wavefront reads (WM + WN) / (WM WN) KiB from LDS, 0.5 KiB at 4 x 4: four
 // wavefronts then take half of LDS's 128 bytes a cycle, and the writes a quarter.  At 2 x 2 they would take all of it; that
@@ -100,20 +100,28 @@ __device__ __forceinline__ void tdc_mx4_tile_at(int id, int mt, int nt, int &m, 
     n = r / rows;
 }
 
+// A wavefront's 64 lanes fetch 16 bytes each from where they point into 1 KiB of LDS, lane after lane, past the registers.
+__device__ __forceinline__ void tdc_mx4_fetch(const uint8_t *from, uint8_t *lds)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+}
+
 template <typename T, int WM, int WN, int GM, int GN>
 __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Product q)
 {
     constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, THREADS = 64 * GM * GN;
-    __shared__ __attribute__((aligned(128))) uint8_t codes[2][(BM + BN) * 128];
-    __shared__ uint2 scales[2][BM + BN];
-    const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6;
+    // two buffers, two objects: a read of one then visibly does not depend on what is being fetched into the other
+    __shared__ __attribute__((aligned(128))) uint8_t codes0[(BM + BN) * 128], codes1[(BM + BN) * 128];
+    __shared__ uint2 scales0[BM + BN], scales1[BM + BN];
+    const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
     tdc_mx4_tile_at(blockIdx.x, (q.M + BM - 1) / BM, (q.N + BN - 1) / BN, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
 
-    // fetch: rows tid/8 + 32 i of both operands, block tid%8 of the eight; scales of rows tid + 256 i
-    constexpr int STEP = THREADS / 8, FA = BM / STEP, FB = BN / STEP, SR = (BM + BN + THREADS - 1) / THREADS;
-    const int fr = tid >> 3, fk = tid & 7;
+    // fetch: rows tid/8 + STEP i of both operands, the block that belongs at place tid%8 of the eight; scales of rows tid + THREADS i
+    constexpr int STEP = THREADS / 8, FA = BM / STEP, FB = BN / STEP, SR = (BM + BN) / THREADS;
+    static_assert((BM + BN) % THREADS == 0 && STEP % 16 == 0, "every thread fetches the same share");
+    const int fr = tid >> 3, fk = (tid & 7) ^ ((fr >> 1) & 7);
     const uint8_t *src[FA + FB], *ssrc[SR];
 #pragma unroll
     for (int i = 0; i < FA; ++i) src[i] = q.a_codes + (size_t)q.a_rows.source(min(m0 + fr + STEP * i, q.M - 1)) * q.nb * 16;
@@ -124,21 +132,20 @@ __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Pr
         const int r = tid + THREADS * i;
         ssrc[i] = r < BM ? q.a_scales + (size_t)q.a_rows.source(min(m0 + r, q.M - 1)) * q.nb : q.b_scales + (size_t)min(n0 + r - BM, q.N - 1) * q.nb;
     }
-    tdc_i4 in[FA + FB];
     uint2 sin[SR];
-    auto fetch = [&](int k) {
+    auto fetch = [&](int k, uint8_t *codes) {
         const size_t at = (size_t)min(k + fk, q.nb - 1) * 16;
 #pragma unroll
-        for (int i = 0; i < FA + FB; ++i) in[i] = *reinterpret_cast<const tdc_i4 *>(src[i] + at);
+        for (int i = 0; i < FA + FB; ++i) tdc_mx4_fetch(src[i] + at, codes + (i * STEP + 8 * wave) * 128);
 #pragma unroll
         for (int i = 0; i < SR; ++i) sin[i] = tdc_mx4_scales8(ssrc[i], k, q.nb);
     };
-    const int wslot = fr * 128 + ((fk ^ ((fr >> 1) & 7)) << 4);
-    auto put = [&](int buf) {
+    // what was fetched is there for every wavefront
+    auto arrive = [&](uint2 *scales) {
 #pragma unroll
-        for (int i = 0; i < FA + FB; ++i) *reinterpret_cast<tdc_i4 *>(&codes[buf][wslot + i * STEP * 128]) = in[i];
-#pragma unroll
-        for (int i = 0; i < SR; ++i) scales[buf][tid + THREADS * i] = sin[i];
+        for (int i = 0; i < SR; ++i) scales[tid + THREADS * i] = sin[i];
+        __builtin_amdgcn_s_waitcnt(0x0070);    // vmcnt(0), lgkmcnt(0)
+        __syncthreads();
     };
 
     const int r32 = l & 31, h = l >> 5, wm = (wave / GN) * 32 * WM, wn = (wave % GN) * 32 * WN;
@@ -150,21 +157,21 @@ __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Pr
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    auto multiply = [&](int buf) {
+    auto multiply = [&](const uint8_t *codes, const uint2 *scales) {
         unsigned sa[WM][2], sb[WN][2];
 #pragma unroll
         for (int i = 0; i < WM; ++i) {
-            const uint2 v = scales[buf][wm + 32 * i + r32];
+            const uint2 v = scales[wm + 32 * i + r32];
             sa[i][0] = v.x >> (8 * h);
             sa[i][1] = v.y >> (8 * h);
         }
 #pragma unroll
         for (int j = 0; j < WN; ++j) {
-            const uint2 v = scales[buf][BM + wn + 32 * j + r32];
+            const uint2 v = scales[BM + wn + 32 * j + r32];
             sb[j][0] = v.x >> (8 * h);
             sb[j][1] = v.y >> (8 * h);
         }
-        const uint8_t *pa = &codes[buf][(wm + r32) * 128], *pb = &codes[buf][(BM + wn + r32) * 128];
+        const uint8_t *pa = codes + (wm + r32) * 128, *pb = codes + (BM + wn + r32) * 128;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int at = ((2 * s + h) ^ ((r32 >> 1) & 7)) << 4;
@@ -181,24 +188,24 @@ __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Pr
         }
     };
 
-    fetch(0);
-    put(0);
-    __syncthreads();
-    int buf = 0;
-    for (int k = 8; k < q.nb; k += 8) {
-        fetch(k);
-        multiply(buf);
-        buf ^= 1;
-        put(buf);
-        __syncthreads();
+    fetch(0, codes0);
+    arrive(scales0);
+    for (int k = 0;; k += 16) {
+        if (k + 8 < q.nb) fetch(k + 8, codes1);
+        multiply(codes0, scales0);
+        if (k + 8 >= q.nb) break;
+        arrive(scales1);
+        if (k + 16 < q.nb) fetch(k + 16, codes0);
+        multiply(codes1, scales1);
+        if (k + 16 >= q.nb) break;
+        arrive(scales0);
     }
-    multiply(buf);
 
     // 32 rows at a time through a piece of LDS of the wavefront's own, so that stores are rows of whole lines.  A pitch of 8 more
     // than a multiple of 32 keeps the two halves of a wavefront, four rows apart, on different banks.
     constexpr int COLS = 32 * WN, PITCH = COLS + 8;
-    static_assert(GM * GN * 32 * PITCH * sizeof(float) <= sizeof(codes), "the sums fit where the codes were");
-    float *sums = reinterpret_cast<float *>(&codes[0][0]) + wave * 32 * PITCH;
+    static_assert(GM * GN / 2 * 32 * PITCH * sizeof(float) <= sizeof(codes0), "the sums fit where the codes were");
+    float *sums = reinterpret_cast<float *>(wave & 1 ? codes1 : codes0) + wave / 2 * 32 * PITCH;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < WM; ++i) {
