@@ -49,9 +49,15 @@ hipError_t tdc_launch_mx4_product(const TdcMx4Product &given, int dtype, hipStre
     TdcMx4Product q = given;
     q.vec = q.N % (16 / tdc_dtype_bytes(dtype)) == 0 && tdc_aligned_to(q.y, 16) && tdc_aligned_to(q.epi.residual, 16);
     const int64_t large = up(q.M, 256) * up(q.N, 256), small = up(q.M, 128) * up(q.N, 128), tiles = up(q.M, 32) * up(q.N, 32);
+    const bool packed = q.nb % 16 == 0 && tdc_aligned_to(q.a_scales, 16) && tdc_aligned_to(q.b_scales, 16);
     TDC_FOR_DTYPE(dtype, T, {
-        if (large >= 128) tdc_mx4_product_tile<T, 4, 2, 2, 4><<<(unsigned)large, 512, 0, s>>>(q);
-        else if (small >= 64) tdc_mx4_product_tile<T, 2, 2, 2, 2><<<(unsigned)small, 256, 0, s>>>(q);
+        if (large >= 128) {
+            if (packed) tdc_mx4_product_tile<T, 4, 2, 2, 4, true><<<(unsigned)large, 512, 0, s>>>(q);
+            else tdc_mx4_product_tile<T, 4, 2, 2, 4, false><<<(unsigned)large, 512, 0, s>>>(q);
+        } else if (small >= 64) {
+            if (packed) tdc_mx4_product_tile<T, 2, 2, 2, 2, true><<<(unsigned)small, 256, 0, s>>>(q);
+            else tdc_mx4_product_tile<T, 2, 2, 2, 2, false><<<(unsigned)small, 256, 0, s>>>(q);
+        }
         else tdc_mx4_product_simple<T><<<(unsigned)((tiles + 3) / 4), 256, 0, s>>>(q);
     });
     return hipGetLastError();

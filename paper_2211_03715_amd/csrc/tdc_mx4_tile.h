@@ -1,19 +1,23 @@
 // Products in tiles through LDS, for operands with many rows on both sides (tdc_mx4_product.hip).
 //
-// Four wavefronts, two by two, share a tile of 64 WM x 64 WN outputs; each computes WM x WN blocks of 32 x 32.  A step takes 256
-// values of k, 128 bytes of codes to a row: a wavefront's fetch covers eight rows of one cache line each.  In LDS a row keeps
-// its 128 bytes, its eight blocks of 16 bytes in the order (block ^ row % 8), so that the eight rows that one pass of a 16-byte
-// read covers fall on different banks.  The next step's codes go straight to the other of two buffers while this step
-// multiplies, its scales through a register: one barrier to a step.
+// GM x GN wavefronts share a tile; each computes WM x WN blocks of 32 x 32.  A step takes 256 values of k, 128 bytes of codes to
+// a row: a wavefront's fetch covers eight rows of one cache line each, straight from memory to LDS.  In LDS a row keeps its
+// eight blocks of 16 bytes in the order (block ^ row/2 % 8), so that sixteen neighbouring rows fall on all 64 banks.  The next
+// step's codes go to the other of two buffers while this step multiplies: one barrier to a step.
 //
-// Per matrix instruction (32 cycles for 64 kFLOP) a wavefront reads (WM + WN) / (WM WN) KiB from LDS, 0.5 KiB at 4 x 4: four
-// wavefronts then take half of LDS's 128 bytes a cycle, and the writes a quarter.  At 2 x 2 they would take all of it; that
-// form is for products too small to fill the chip with the large one.
+// Scales are a byte to 16 bytes of codes but as many cache lines as there are rows, and the L1 takes a cycle for each line:
+// 8 bytes to a row and step, they would take half as long as the codes.  Where the rows' scales are whole pieces of 16 bytes
+// (PACKED) they are fetched for four steps at once, two lanes to a row, and read from LDS for two.
 //
-// Blocks of k past the end: the fetch reads the last block again, and both scales are zero bytes, 2^-127 each, so that what
-// comes of them, below 2^-243, is lost in any fp32 sum.
+// Per matrix instruction (32 cycles for 131 kFLOP) a wavefront reads (WM + WN) / (WM WN) KiB from LDS: 3/4 KiB at 4 x 2, with
+// four such streams at a time three quarters of LDS's 128 bytes a cycle.
+//
+// Blocks of k past the end exist only where PACKED is false: the fetch reads the last block again, and both scales are zero
+// bytes, 2^-127 each, so that what comes of them, below 2^-243, is lost in any fp32 sum.
 #ifndef TDC_MX4_TILE_H
 #define TDC_MX4_TILE_H
+
+#include <type_traits>
 
 #include "tdc_mx4_internal.h"
 
@@ -106,44 +110,56 @@ __device__ __forceinline__ void tdc_mx4_fetch(const uint8_t *from, uint8_t *lds)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
 
-template <typename T, int WM, int WN, int GM, int GN>
+template <typename T, int WM, int WN, int GM, int GN, bool PACKED>
 __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Product q)
 {
-    constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, THREADS = 64 * GM * GN;
-    // two buffers, two objects: a read of one then visibly does not depend on what is being fetched into the other
-    __shared__ __attribute__((aligned(128))) uint8_t codes0[(BM + BN) * 128], codes1[(BM + BN) * 128];
-    __shared__ uint2 scales0[BM + BN], scales1[BM + BN];
+    constexpr int BM = 32 * WM * GM, BN = 32 * WN * GN, ROWS = BM + BN, THREADS = 64 * GM * GN, WAVES = GM * GN;
+    // separate objects: a read of one buffer then visibly does not depend on what is being fetched into the other
+    __shared__ __attribute__((aligned(1024))) uint8_t codes0[ROWS * 128], codes1[ROWS * 128];
+    __shared__ __attribute__((aligned(1024))) uint8_t scales[2][ROWS * (PACKED ? 32 : 8)];
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
     tdc_mx4_tile_at(blockIdx.x, (q.M + BM - 1) / BM, (q.N + BN - 1) / BN, tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN;
+    const int m0 = tm * BM, n0 = tn * BN, steps = (q.nb + 7) / 8;
+    auto row_of = [&](int r) { return r < BM ? (size_t)q.a_rows.source(min(m0 + r, q.M - 1)) : (size_t)min(n0 + r - BM, q.N - 1); };
 
-    // fetch: rows tid/8 + STEP i of both operands, the block that belongs at place tid%8 of the eight; scales of rows tid + THREADS i
-    constexpr int STEP = THREADS / 8, FA = BM / STEP, FB = BN / STEP, SR = (BM + BN) / THREADS;
-    static_assert((BM + BN) % THREADS == 0 && STEP % 16 == 0, "every thread fetches the same share");
+    // codes: rows tid/8 + STEP i of both operands, the block that belongs at place tid%8 of the eight
+    constexpr int STEP = THREADS / 8, F = ROWS / STEP;
+    static_assert(BM % STEP == 0 && BN % STEP == 0 && STEP % 16 == 0, "every thread fetches the same share");
     const int fr = tid >> 3, fk = (tid & 7) ^ ((fr >> 1) & 7);
-    const uint8_t *src[FA + FB], *ssrc[SR];
+    const uint8_t *src[F];
 #pragma unroll
-    for (int i = 0; i < FA; ++i) src[i] = q.a_codes + (size_t)q.a_rows.source(min(m0 + fr + STEP * i, q.M - 1)) * q.nb * 16;
+    for (int i = 0; i < F; ++i) src[i] = (STEP * i < BM ? q.a_codes : q.b_codes) + row_of(fr + STEP * i) * q.nb * 16;
+    auto fetch = [&](int t, uint8_t *codes) {
+        const size_t at = (size_t)(PACKED ? 8 * t + fk : min(8 * t + fk, q.nb - 1)) * 16;
 #pragma unroll
-    for (int i = 0; i < FB; ++i) src[FA + i] = q.b_codes + (size_t)min(n0 + fr + STEP * i, q.N - 1) * q.nb * 16;
+        for (int i = 0; i < F; ++i) tdc_mx4_fetch(src[i] + at, codes + (i * STEP + 8 * wave) * 128);
+    };
+
+    // scales, PACKED: rows 32 wave + l/2 + 32 WAVES i, 16 bytes to a lane; of the two pieces the second comes first in eight of sixteen
+    // rows.  Otherwise: rows tid + THREADS i, eight bytes through a register.
+    constexpr int SR = PACKED ? ROWS / (32 * WAVES) : ROWS / THREADS;
+    const uint8_t *ssrc[SR];
+    uint2 sin[PACKED ? 1 : SR];
+    const int sr = 32 * wave + (l >> 1), sk = (l & 1) ^ ((l >> 4) & 1);
 #pragma unroll
     for (int i = 0; i < SR; ++i) {
-        const int r = tid + THREADS * i;
-        ssrc[i] = r < BM ? q.a_scales + (size_t)q.a_rows.source(min(m0 + r, q.M - 1)) * q.nb : q.b_scales + (size_t)min(n0 + r - BM, q.N - 1) * q.nb;
+        const int r = PACKED ? sr + 32 * WAVES * i : tid + THREADS * i;
+        ssrc[i] = (r < BM ? q.a_scales : q.b_scales) + row_of(r) * q.nb;
     }
-    uint2 sin[SR];
-    auto fetch = [&](int k, uint8_t *codes) {
-        const size_t at = (size_t)min(k + fk, q.nb - 1) * 16;
+    auto fetch_scales = [&](int chunk) {    // PACKED: of steps 4 chunk .. 4 chunk + 3, whose second half may be past the end
+        const int at = min(2 * chunk + sk, q.nb / 16 - 1) * 16;
 #pragma unroll
-        for (int i = 0; i < FA + FB; ++i) tdc_mx4_fetch(src[i] + at, codes + (i * STEP + 8 * wave) * 128);
+        for (int i = 0; i < SR; ++i) tdc_mx4_fetch(ssrc[i] + at, &scales[chunk & 1][32 * (32 * wave + 32 * WAVES * i)]);
+    };
+    auto load_scales = [&](int t) {         // otherwise: of step t
 #pragma unroll
-        for (int i = 0; i < SR; ++i) sin[i] = tdc_mx4_scales8(ssrc[i], k, q.nb);
+        for (int i = 0; i < SR && !PACKED; ++i) sin[i] = tdc_mx4_scales8(ssrc[i], 8 * t, q.nb);
     };
     // what was fetched is there for every wavefront
-    auto arrive = [&](uint2 *scales) {
+    auto arrive = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < SR; ++i) scales[tid + THREADS * i] = sin[i];
+        for (int i = 0; i < SR && !PACKED; ++i) *reinterpret_cast<uint2 *>(&scales[t & 1][8 * (tid + THREADS * i)]) = sin[i];
         __builtin_amdgcn_s_waitcnt(0x0070);    // vmcnt(0), lgkmcnt(0)
         __syncthreads();
     };
@@ -157,20 +173,26 @@ __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Pr
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    auto multiply = [&](const uint8_t *codes, const uint2 *scales) {
-        unsigned sa[WM][2], sb[WN][2];
+    // Scales of two steps (PACKED) or of one in registers, shifted so that bytes 0 and 2 are those of the lane's blocks.
+    constexpr int SW = PACKED ? 4 : 2;
+    unsigned sa[WM][SW], sb[WN][SW];
+    auto read_scales = [&](int t) {
+        auto read = [&](int r, unsigned (&s)[SW]) {
+            if constexpr (PACKED) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(&scales[(t >> 2) & 1][32 * r + 16 * (((t >> 1) & 1) ^ ((r32 >> 3) & 1))]);
+                s[0] = v.x >> (8 * h), s[1] = v.y >> (8 * h), s[2] = v.z >> (8 * h), s[3] = v.w >> (8 * h);
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2 *>(&scales[t & 1][8 * r]);
+                s[0] = v.x >> (8 * h), s[1] = v.y >> (8 * h);
+            }
+        };
 #pragma unroll
-        for (int i = 0; i < WM; ++i) {
-            const uint2 v = scales[wm + 32 * i + r32];
-            sa[i][0] = v.x >> (8 * h);
-            sa[i][1] = v.y >> (8 * h);
-        }
+        for (int i = 0; i < WM; ++i) read(wm + 32 * i + r32, sa[i]);
 #pragma unroll
-        for (int j = 0; j < WN; ++j) {
-            const uint2 v = scales[BM + wn + 32 * j + r32];
-            sb[j][0] = v.x >> (8 * h);
-            sb[j][1] = v.y >> (8 * h);
-        }
+        for (int j = 0; j < WN; ++j) read(BM + wn + 32 * j + r32, sb[j]);
+    };
+    auto multiply = [&](const uint8_t *codes, auto second) {
+        constexpr int W = decltype(second)::value && PACKED ? 2 : 0;
         const uint8_t *pa = codes + (wm + r32) * 128, *pb = codes + (BM + wn + r32) * 128;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -184,21 +206,33 @@ __global__ __launch_bounds__(64 * GM * GN, 2) void tdc_mx4_product_tile(TdcMx4Pr
             for (int i = 0; i < WM; ++i)
 #pragma unroll
                 for (int j = 0; j < WN; ++j)
-                    acc[i][j] = s & 1 ? tdc_mx4_mfma<2>(a[i], sa[i][s / 2], b[j], sb[j][s / 2], acc[i][j]) : tdc_mx4_mfma<0>(a[i], sa[i][s / 2], b[j], sb[j][s / 2], acc[i][j]);
+                    acc[i][j] = s & 1 ? tdc_mx4_mfma<2>(a[i], sa[i][W + s / 2], b[j], sb[j][W + s / 2], acc[i][j]) : tdc_mx4_mfma<0>(a[i], sa[i][W + s / 2], b[j], sb[j][W + s / 2], acc[i][j]);
         }
     };
 
     fetch(0, codes0);
-    arrive(scales0);
-    for (int k = 0;; k += 16) {
-        if (k + 8 < q.nb) fetch(k + 8, codes1);
-        multiply(codes0, scales0);
-        if (k + 8 >= q.nb) break;
-        arrive(scales1);
-        if (k + 16 < q.nb) fetch(k + 16, codes0);
-        multiply(codes1, scales1);
-        if (k + 16 >= q.nb) break;
-        arrive(scales0);
+    if constexpr (PACKED) fetch_scales(0);
+    else load_scales(0);
+    arrive(0);
+    for (int t = 0;; t += 2) {
+        // scales first: what is fetched into their array from here on must not be waited for by their reads
+        read_scales(t);
+        if (t + 1 < steps) {
+            fetch(t + 1, codes1);
+            if constexpr (!PACKED) load_scales(t + 1);
+            else if ((t & 3) == 0 && t + 4 < steps) fetch_scales(t / 4 + 1);
+        }
+        multiply(codes0, std::false_type());
+        if (t + 1 >= steps) break;
+        arrive(t + 1);
+        if constexpr (!PACKED) read_scales(t + 1);
+        if (t + 2 < steps) {
+            fetch(t + 2, codes0);
+            if constexpr (!PACKED) load_scales(t + 2);
+        }
+        multiply(codes1, std::true_type());
+        if (t + 2 >= steps) break;
+        arrive(t + 2);
     }
 
     // 32 rows at a time through a piece of LDS of the wavefront's own, so that stores are rows of whole lines.  A pitch of 8 more

@@ -107,7 +107,9 @@ def _product(av, bv, bias, res, act, K):
 # M, N, K: one of each, borders of blocks and tiles, one row, few rows, few columns, long sums, more than a tile each way
 PRODUCTS = [(1, 1, 1), (1, 1000, 2048), (1, 33, 8192), (2, 16, 32), (3, 17, 65), (16, 64, 512), (17, 129, 100), (31, 31, 31), (33, 40, 96), (64, 256, 256), (65, 257, 160),
             (100, 10, 300), (127, 130, 1000), (128, 128, 2080), (300, 520, 768), (512, 1024, 1024), (1000, 300, 4096), (4, 2000, 4100), (700, 64, 64), (2049, 129, 33), (257, 513, 8200),
-            (1024, 768, 256), (48, 4096, 544), (515, 772, 1280)]
+            (1024, 768, 256), (48, 4096, 544), (515, 772, 1280),
+            # large tiles and smaller ones, from one step of k to many, with whole and broken groups of four blocks
+            (1100, 1030, 20), (1100, 1030, 250), (1152, 1024, 384), (1030, 1100, 544), (1025, 1300, 1000), (2900, 3000, 100), (3000, 2817, 33), (2817, 3000, 512), (2900, 2900, 1300)]
 
 
 @pytest.mark.parametrize("shape", PRODUCTS, ids=lambda s: "x".join(map(str, s)))
