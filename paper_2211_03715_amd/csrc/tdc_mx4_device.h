@@ -23,7 +23,7 @@ __device__ __forceinline__ unsigned tdc_mx4_scale(unsigned top)
     return field == 255u ? 255u : (field > 2u ? field - 2u : 0u);
 }
 
-// Eight values, in units of 2^(e - 127), as eight codes.  The conversion takes its scale from the exponent field of a float, 0
+// Eight values (four below), in units of 2^(e - 127), as eight codes.  The conversion takes its scale from the exponent field of a float, 0
 // for 2^-127, rounds to nearest even and saturates: checked for every e at every border between codes and its neighbours.
 __device__ __forceinline__ unsigned tdc_mx4_codes8(const float *v, unsigned e)
 {
@@ -33,6 +33,15 @@ __device__ __forceinline__ unsigned tdc_mx4_codes8(const float *v, unsigned e)
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+    return e == 255u ? 0u : c;
+}
+
+__device__ __forceinline__ unsigned tdc_mx4_codes4(const float *v, unsigned e)
+{
+    const float scale = __builtin_bit_cast(float, e << 23);
+    unsigned c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
     return e == 255u ? 0u : c;
 }
 

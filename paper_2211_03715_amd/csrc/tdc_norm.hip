@@ -1,6 +1,5 @@
 // Group norm with an activation, channels last: plans, the forward kernels and their launches (tdc_norm.h).
 #include <cmath>
-#include <initializer_list>
 #include <new>
 
 #include "tdc_mx4_device.h"
@@ -8,150 +7,199 @@
 
 namespace {
 
-// ---- statistics of a chunk: grid (chunks, batch)
-//
-// A thread takes its V channels of eight pixels at a time into registers, their mean and the squares about it, and merges that
-// into what it has (n_a, mean_a, S_a with n_b, mean_b, S_b: mean = mean_a + d n_b / n, S = S_a + S_b + d^2 n_a n_b / n,
-// d = mean_b - mean_a).  No sum of squares is ever taken about anything but a mean next to the values, so fp32 does.
+// Where a forward call's results go.
+struct NormOut {
+    void *y;                 // or null:
+    uint8_t *codes, *scales;
+    int64_t pitch;
+    float *mean, *rstd;      // or null
+};
+
+struct NormIn {
+    const void *x, *residual;
+    const float *gamma, *beta;
+    int64_t xp, rp;
+    int act;                 // the same for every thread: a branch to V values costs next to nothing beside their way to memory
+};
+
+// Constants of a thread's V channels.
+template <int V> struct Affine {
+    float mean[V], scale[V], shift[V];
+    // stats: of the groups from g0 on
+    __device__ __forceinline__ void set(const TdcNormDims &d, const NormIn &in, const float2 *stats, int g0, int c0)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float2 st = stats[(c0 + v) / d.Cg - g0];
+            mean[v] = st.x;
+            scale[v] = in.gamma ? st.y * in.gamma[c0 + v] : st.y;
+            shift[v] = in.beta ? in.beta[c0 + v] : 0.f;
+        }
+    }
+};
+
 template <typename T, int V>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_stats(TdcNormDims d, const T *__restrict__ x, int64_t pitch, float2 *__restrict__ partial)
+__device__ __forceinline__ void apply(const Affine<V> &k, const TdcVec<T, V> &x, const TdcVec<T, V> &res, const NormIn &in, float (&o)[V])
 {
-    constexpr int U = 8;
-    extern __shared__ float2 chan[];                       // [rows][C]
-    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x;
-    const int len = tdc_chunk_len(d, chunk);
-    const int rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-    const int r = threadIdx.x / nv, step = nv <= TDC_NORM_THREADS ? nv : TDC_NORM_THREADS;
-    const T *base = x + ((size_t)b * d.P + (size_t)chunk * d.chunk_px) * pitch;
-    if (rows == 1 || r < rows)
-        for (int cv = rows == 1 ? threadIdx.x : threadIdx.x - r * nv; cv < nv; cv += step) {
-            float n = 0.f, mean[V], m2[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.f;
-            for (int p = rows == 1 ? 0 : r; p < len; p += rows * U) {
-                TdcVec<T, V> in[U];
+    for (int v = 0; v < V; ++v) o[v] = ((float)x.v[v] - k.mean[v]) * k.scale[v] + k.shift[v];
+    if (in.residual) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) in[u] = tdc_load<T, V>(base + (size_t)min(p + u * rows, len - 1) * pitch + cv * V);
-                const int k = min(U, (len - p + rows - 1) / rows);
-                const float inv_k = 1.f / k, tot = n + k, w = k / tot;
+        for (int v = 0; v < V; ++v) o[v] += (float)res.v[v];
+    }
+    tdc_activate_all(in.act, o);
+}
+
+// V of a block's 32 channels to a lane, 32 / V neighbouring lanes to a block: all of them call this, `live` or not.
+template <int V> __device__ __forceinline__ void store_mx4(const NormOut &out, const float (&o)[V], size_t px, int nb, int c0, bool live)
+{
+    unsigned top = 0;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float s = 0.f, q = 0.f;
+    for (int v = 0; v < V; ++v) top = max(top, tdc_abs_bits(o[v]));
 #pragma unroll
-                    for (int u = 0; u < U; ++u) s += u < k ? (float)in[u].v[v] : 0.f;
-                    s *= inv_k;
+    for (int l = 1; l < 32 / V; l <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, l, 64));
+    const unsigned e = tdc_mx4_scale(top);
+    if (!live) return;
+    const size_t block = px * nb + c0 / 32;
+    uint8_t *at = out.codes + block * 16 + (c0 % 32) / 2;
+    if constexpr (V == 8) *reinterpret_cast<unsigned *>(at) = tdc_mx4_codes8(o, e);
+    else *reinterpret_cast<uint16_t *>(at) = (uint16_t)tdc_mx4_codes4(o, e);
+    if (c0 % 32 == 0) out.scales[block] = (uint8_t)e;
+}
+
+// ---- resident: a slice of an image's channels in the registers of a workgroup
+template <typename T, int V, bool WHOLE, bool MX4, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void tdc_norm_resident(TdcNormDims d, NormIn in, NormOut out, int width, int slices)
+{
+    __shared__ float2 items[THREADS * (WHOLE ? 1 : V)], stats[THREADS];
+    int b, slice;
+    tdc_norm_place(blockIdx.x, gridDim.x, slices, b, slice);
+    const int nv = width / V, groups = width / d.Cg, c0 = slice * width;
+    const TdcNormLanes t(nv, THREADS);
+    const bool live = t.r < t.rows && t.cv < nv;
+    const T *x = static_cast<const T *>(in.x) + (size_t)b * d.P * in.xp + c0 + t.cv * V;
+    TdcVec<T, V> held[HELD];
+    const int k = live && t.r < d.P ? (d.P - t.r + t.rows - 1) / t.rows : 0;   // pixels of this thread
+    if (k) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const float off = u < k ? (float)in[u].v[v] - s : 0.f;
-                        q += off * off;
-                    }
-                    const float off = s - mean[v];
-                    mean[v] += off * w;
-                    m2[v] += q + off * off * (n * w);
-                }
-                n = tot;
+        for (int i = 0; i < HELD; ++i) held[i] = tdc_load<T, V>(x + (size_t)min(t.r + i * t.rows, d.P - 1) * in.xp);
+        TdcNormSums<V> sums;
+        sums.add(held, k);
+        sums.template put<WHOLE>(items, t.r, nv, t.cv);
+    }
+    __syncthreads();
+    const size_t at = (size_t)b * d.G + c0 / d.Cg;
+    tdc_norm_groups(items, min(t.rows, d.P), d.P / t.rows, d.P % t.rows, groups, WHOLE ? d.Cg / V : d.Cg, WHOLE ? V : 1, THREADS, [&](int g, float n, float mean, float m2) {
+        const float rstd = tdc_rstd(m2 / n, d.eps);
+        stats[g] = make_float2(mean, rstd);
+        if (out.mean) out.mean[at + g] = mean;
+        if (out.rstd) out.rstd[at + g] = rstd;
+    });
+    __syncthreads();
+    if (!live && !MX4) return;
+    Affine<V> a;
+    a.set(d, in, stats, c0 / d.Cg, c0 + (live ? t.cv * V : 0));
+    const T *res = in.residual ? static_cast<const T *>(in.residual) + (size_t)b * d.P * in.rp + c0 + t.cv * V : nullptr;
+    // MX4: lanes that share a block have the same pixels, but their neighbours in the wavefront may have one less
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int p = tdc_anew(t.r + i * t.rows);
+        const bool mine = live && p < d.P;
+        if (!mine && !MX4) break;
+        tdc_forget(held[i]);
+        TdcVec<T, V> rv;
+        if (res && mine) rv = tdc_load<T, V>(res + (size_t)p * in.rp);
+        float o[V];
+        apply(a, held[i], rv, in, o);
+        const size_t px = (size_t)b * d.P + p;
+        if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
+        else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
+    }
+}
+
+// ---- statistics of a chunk: grid (chunks, batch)
+template <typename T, int V, bool WHOLE>
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_stats(TdcNormDims d, NormIn in, float4 *__restrict__ partial)
+{
+    constexpr int U = TDC_NORM_UNROLL;
+    extern __shared__ float2 items[];
+    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
+    const TdcNormLanes t(nv, TDC_NORM_THREADS);
+    const T *base = static_cast<const T *>(in.x) + ((size_t)b * d.P + (size_t)chunk * d.chunk_px) * in.xp;
+    if (t.r < min(t.rows, len))
+        for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
+            TdcNormSums<V> sums;
+            for (int p = t.r; p < len; p += t.rows * U) {
+                TdcVec<T, V> v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(base + (size_t)min(p + u * t.rows, len - 1) * in.xp + cv * V);
+                sums.add(v, min(U, (len - p + t.rows - 1) / t.rows));
             }
-#pragma unroll
-            for (int v = 0; v < V; ++v) chan[(rows == 1 ? 0 : r) * d.C + cv * V + v] = make_float2(mean[v], m2[v]);
-            if (rows > 1) break;
+            sums.template put<WHOLE>(items, t.r, nv, cv);
+            if (t.rows > 1) break;
         }
     __syncthreads();
-    // rows of the workgroup into one, channel by channel
-    const int used = min(rows, len);
-    if (used > 1) {
-        for (int c = threadIdx.x; c < d.C; c += TDC_NORM_THREADS) {
-            float n = 0.f, mean = 0.f, m2 = 0.f;
-            for (int i = 0; i < used; ++i) {
-                const float2 o = chan[i * d.C + c];
-                const float k = (float)((len - i + rows - 1) / rows), tot = n + k, off = o.x - mean;
-                mean += off * (k / tot);
-                m2 += o.y + off * off * (n * (k / tot));
-                n = tot;
-            }
-            chan[c] = make_float2(mean, m2);
-        }
-        __syncthreads();
-    }
-    // channels into groups, a team of lanes to a group
-    const int L = tdc_team(d.G, d.Cg), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = TDC_NORM_THREADS / L;
-    for (int g0 = 0; g0 < d.G; g0 += teams) {
-        const int g = min(g0 + team, d.G - 1);
-        float s = 0.f, m2 = 0.f;
-        for (int c = lane; c < d.Cg; c += L) s += chan[g * d.Cg + c].x;
-        const float mean = tdc_lane_sum(s, L) / d.Cg;
-        for (int c = lane; c < d.Cg; c += L) {
-            const float2 o = chan[g * d.Cg + c];
-            m2 += o.y + (o.x - mean) * (o.x - mean) * len;
-        }
-        m2 = tdc_lane_sum(m2, L);
-        if (lane == 0 && g0 + team < d.G) partial[((size_t)b * d.chunks + chunk) * d.G + g] = make_float2(mean, m2);
-    }
+    float4 *out = partial + ((size_t)b * d.chunks + chunk) * d.G;
+    tdc_norm_groups(items, min(t.rows, len), len / t.rows, len % t.rows, d.G, WHOLE ? d.Cg / V : d.Cg, WHOLE ? V : 1, TDC_NORM_THREADS,
+                    [&](int g, float n, float mean, float m2) { out[g] = make_float4(n, mean, m2, 0.f); });
 }
 
 // ---- y = act((x - mean) * (rstd gamma) + beta + residual): grid (chunks, batch)
-template <typename T, int V, int ACT>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d, const T *__restrict__ x, int64_t xp, const float *__restrict__ gamma,
-                                                                    const float *__restrict__ beta, const T *__restrict__ res, int64_t rp, T *__restrict__ y,
-                                                                    int64_t yp, const float2 *__restrict__ partial, float *__restrict__ mean_out, float *__restrict__ rstd_out)
+template <typename T, int V, bool MX4>
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial)
 {
+    constexpr int U = TDC_NORM_UNROLL;
     extern __shared__ float2 stats[];                      // [G]
-    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x;
-    tdc_combine_chunks(d, partial, b, stats);
+    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
+    tdc_combine_chunks(d, partial, b, stats, TDC_NORM_THREADS);
     if (chunk == 0)
         for (int g = threadIdx.x; g < d.G; g += TDC_NORM_THREADS) {
-            if (mean_out) mean_out[(size_t)b * d.G + g] = stats[g].x;
-            if (rstd_out) rstd_out[(size_t)b * d.G + g] = stats[g].y;
+            if (out.mean) out.mean[(size_t)b * d.G + g] = stats[g].x;
+            if (out.rstd) out.rstd[(size_t)b * d.G + g] = stats[g].y;
         }
-    const int len = tdc_chunk_len(d, chunk);
-    const int rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-    const int r = rows == 1 ? 0 : threadIdx.x / nv;
-    if (r >= rows) return;
+    const TdcNormLanes t(nv, TDC_NORM_THREADS);
     const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
-    for (int cv = rows == 1 ? threadIdx.x : threadIdx.x - r * nv; cv < nv; cv += TDC_NORM_THREADS) {
-        float mean[V], a[V], shift[V];
+    const T *x = static_cast<const T *>(in.x) + first * in.xp, *res = in.residual ? static_cast<const T *>(in.residual) + first * in.rp : nullptr;
+    // MX4: the lanes of a block go through the loops together (nv is a multiple of 32 / V)
+    if (t.r >= t.rows) return;
+    for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
+        Affine<V> a;
+        a.set(d, in, stats, 0, cv * V);
+        for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
+            TdcVec<T, V> v[U], rv[U];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = cv * V + v;
-            const float2 st = stats[c / d.Cg];
-            mean[v] = st.x;
-            a[v] = gamma ? st.y * gamma[c] : st.y;
-            shift[v] = beta ? beta[c] : 0.f;
-        }
-        for (int p = r; p < len; p += rows) {
-            const size_t px = first + p;
-            const TdcVec<T, V> in = tdc_load<T, V>(x + px * xp + cv * V);
-            float o[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) o[v] = ((float)in.v[v] - mean[v]) * a[v] + shift[v];
+            for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(x + (size_t)min(p0 + u * t.rows, len - 1) * in.xp + cv * V);
             if (res) {
-                const TdcVec<T, V> rv = tdc_load<T, V>(res + px * rp + cv * V);
 #pragma unroll
-                for (int v = 0; v < V; ++v) o[v] += (float)rv.v[v];
+                for (int u = 0; u < U; ++u) rv[u] = tdc_load<T, V>(res + (size_t)min(p0 + u * t.rows, len - 1) * in.rp + cv * V);
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) o[v] = tdc_activate<ACT>(o[v]);
-            tdc_store<T, V>(y + px * yp + cv * V, o);
+            for (int u = 0; u < U; ++u) {
+                const int p = p0 + u * t.rows;
+                float o[V];
+                apply(a, v[u], rv[u], in, o);
+                if constexpr (MX4) store_mx4<V>(out, o, first + p, (d.C + 31) / 32, cv * V, p < len);
+                else if (p < len) tdc_store<T, V>(static_cast<T *>(out.y) + (first + p) * out.pitch + cv * V, o);
+            }
         }
-        if (rows > 1) break;
+        if (t.rows > 1) break;
     }
 }
 
-// ---- the same, written in 4 bits: a thread takes a block of 32 channels of a pixel
-template <typename T, int V, int ACT>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_mx4(TdcNormDims d, const T *__restrict__ x, int64_t xp, const float *__restrict__ gamma,
-                                                                        const float *__restrict__ beta, const T *__restrict__ res, int64_t rp,
-                                                                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
-                                                                        const float2 *__restrict__ partial, float *__restrict__ mean_out, float *__restrict__ rstd_out)
+// ---- the same, written in 4 bits, where C is no multiple of 32: a thread takes a block of 32 channels of a pixel
+template <typename T, int V>
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_blocks(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial)
 {
     extern __shared__ float2 stats[];                      // [G]
     const int b = blockIdx.y, chunk = blockIdx.x;
-    tdc_combine_chunks(d, partial, b, stats);
+    tdc_combine_chunks(d, partial, b, stats, TDC_NORM_THREADS);
     if (chunk == 0)
         for (int g = threadIdx.x; g < d.G; g += TDC_NORM_THREADS) {
-            if (mean_out) mean_out[(size_t)b * d.G + g] = stats[g].x;
-            if (rstd_out) rstd_out[(size_t)b * d.G + g] = stats[g].y;
+            if (out.mean) out.mean[(size_t)b * d.G + g] = stats[g].x;
+            if (out.rstd) out.rstd[(size_t)b * d.G + g] = stats[g].y;
         }
     const int nb = (d.C + 31) / 32;
+    const T *x = static_cast<const T *>(in.x), *res = static_cast<const T *>(in.residual);
     const size_t total = (size_t)tdc_chunk_len(d, chunk) * nb, first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
     for (size_t i = threadIdx.x; i < total; i += TDC_NORM_THREADS) {
         const size_t px = first + i / nb;
@@ -159,27 +207,23 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_mx4(TdcNormDi
         float o[32];
 #pragma unroll
         for (int j = 0; j < 32; j += V) {
+            float part[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) part[v] = 0.f;
             if (c0 + j < d.C) {                            // V divides C: all of them or none
-                const TdcVec<T, V> in = tdc_load<T, V>(x + px * xp + c0 + j);
+                Affine<V> a;
+                a.set(d, in, stats, 0, c0 + j);
                 TdcVec<T, V> rv;
-                if (res) rv = tdc_load<T, V>(res + px * rp + c0 + j);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int c = c0 + j + v;
-                    const float2 st = stats[c / d.Cg];
-                    float f = ((float)in.v[v] - st.x) * (gamma ? st.y * gamma[c] : st.y) + (beta ? beta[c] : 0.f);
-                    if (res) f += (float)rv.v[v];
-                    o[j + v] = tdc_activate<ACT>(f);
-                }
-            } else {
-#pragma unroll
-                for (int v = 0; v < V; ++v) o[j + v] = 0.f;
+                if (res) rv = tdc_load<T, V>(res + px * in.rp + c0 + j);
+                apply(a, tdc_load<T, V>(x + px * in.xp + c0 + j), rv, in, part);
             }
+#pragma unroll
+            for (int v = 0; v < V; ++v) o[j + v] = part[v];
         }
         unsigned e;
         const tdc_i4 c = tdc_mx4_block(o, e);
-        *reinterpret_cast<tdc_i4 *>(codes + (px * nb + c0 / 32) * 16) = c;
-        scales[px * nb + c0 / 32] = (uint8_t)e;
+        *reinterpret_cast<tdc_i4 *>(out.codes + (px * nb + c0 / 32) * 16) = c;
+        out.scales[px * nb + c0 / 32] = (uint8_t)e;
     }
 }
 
@@ -191,14 +235,13 @@ int validate(const tdc_norm_shape &s)
     return TDC_OK;
 }
 
-// Pixels to a chunk: what keeps eight pieces of 16 bytes in flight for every thread of a workgroup, and more where that would
-// make over 2048 workgroups (8 to a compute unit).
+// Pixels to a chunk: two workgroups to a compute unit over the batch, but no less than one round of a workgroup's threads.
 void choose_chunks(TdcNormDims &d, int dtype)
 {
     const int pieces = (d.C * tdc_dtype_bytes(dtype) + 15) / 16;
     const int rows = pieces < TDC_NORM_THREADS ? TDC_NORM_THREADS / pieces : 1;
-    const int most = d.B >= 2048 ? 1 : 2048 / d.B;
-    const int64_t chunks = std::min<int64_t>(most, (d.P + 8 * rows - 1) / (8 * rows));
+    const int most = d.B >= 512 ? 1 : 512 / d.B;
+    const int64_t chunks = std::min<int64_t>(most, ((int64_t)d.P + TDC_NORM_UNROLL * rows - 1) / (TDC_NORM_UNROLL * rows));
     d.chunk_px = (int)((d.P + chunks - 1) / chunks);
     d.chunks = (d.P + d.chunk_px - 1) / d.chunk_px;
 }
@@ -225,14 +268,15 @@ int tdc_norm_plan_create(tdc_norm_plan **out, const tdc_norm_shape *shape, int d
     p->device = device;
     p->dims = TdcNormDims{shape->batch, shape->H * shape->W, shape->C, shape->groups, shape->C / shape->groups, 0, 0, shape->eps};
     choose_chunks(p->dims, shape->dtype);
-    const size_t pairs = (size_t)p->dims.B * p->dims.chunks * p->dims.C, means = (size_t)p->dims.B * p->dims.G;
-    p->ws_bytes = (pairs + means) * sizeof(float2);
+    const size_t groups = (size_t)p->dims.B * p->dims.G, partials = groups * p->dims.chunks;
+    const size_t sums = std::min<size_t>((size_t)p->dims.B * p->dims.chunks, TDC_NORM_SUM_ROWS) * p->dims.C;
+    p->ws_bytes = partials * sizeof(float4) + sums * sizeof(float2);
     if (hipMalloc((void **)&p->partial, p->ws_bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete p;
         return TDC_ERR_ALLOC;
     }
-    p->means = p->partial + pairs;
+    p->sums = reinterpret_cast<float2 *>(p->partial + partials);
     *out = p;
     return TDC_OK;
 }
@@ -248,7 +292,12 @@ int tdc_norm_plan_destroy(tdc_norm_plan *p)
 
 size_t tdc_norm_plan_workspace_bytes(const tdc_norm_plan *p) { return p ? p->ws_bytes : 0; }
 
-int tdc_norm_plan_kernel_count(const tdc_norm_plan *p) { return p ? 2 : 0; }
+int tdc_norm_plan_kernel_count(const tdc_norm_plan *p)
+{
+    if (!p) return 0;
+    const int V = tdc_norm_vec(p->shape.dtype, p->dims.C, {}, {});
+    return tdc_norm_slice(p->dims, p->shape.dtype, V, false, 1).held ? 1 : 2;
+}
 
 }  // extern "C"
 
@@ -267,18 +316,42 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     if (!tdc_aligned_to(codes, 16)) return TDC_ERR_UNSUPPORTED;
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
+    const NormIn in{x, a.residual, gamma, beta, xp, rp, p->shape.act};
+    const NormOut out{y, codes, scales, yp, a.mean, a.rstd};
+    const int vx = tdc_norm_vec(dt, d.C, {xp}, {x});
+    const int V0 = y ? tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0, yp}, {x, a.residual, y}) : tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0}, {x, a.residual});
+    const bool lanes = codes && d.C % 32 == 0 && V0 * size == 16;     // blocks of 4-bit values over neighbouring lanes
+    const TdcNormSlice sl = y || lanes ? tdc_norm_slice(d, dt, V0, false, lanes ? 32 : 1) : TdcNormSlice{};
+    const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);
+    if (sl.held) {
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC(V0, T, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), false), THREADS, HELD, {
+            const unsigned wgs = (unsigned)d.B * sl.slices;
+            if (lanes) {
+                if constexpr (V * sizeof(T) == 16) {
+                    if (whole) tdc_norm_resident<T, V, true, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+                    else tdc_norm_resident<T, V, false, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+                }
+            } else {
+                if (whole) tdc_norm_resident<T, V, true, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+                else tdc_norm_resident<T, V, false, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+            }
+        })));
+        return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    }
     TDC_FOR_DTYPE(dt, T, {
-        const T *xt = (const T *)x, *rt = (const T *)a.residual;
-        TDC_FOR_VEC(tdc_norm_vec(dt, d.C, {xp}, {x}), T, V, {
-            const int nv = d.C / V, rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-            tdc_norm_stats<T, V><<<grid, TDC_NORM_THREADS, (size_t)rows * d.C * sizeof(float2), s>>>(d, xt, xp, p->partial);
+        TDC_FOR_VEC(vx, T, V, {
+            const int nv = d.C / V, rows = nv < TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
+            const size_t lds = (size_t)rows * (whole_x ? nv : d.C) * sizeof(float2);
+            if (whole_x) tdc_norm_stats<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
+            else tdc_norm_stats<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
         });
-        const int vec = y ? tdc_norm_vec(dt, d.C, {xp, rt ? rp : 0, yp}, {x, rt, y}) : tdc_norm_vec(dt, d.C, {xp, rt ? rp : 0}, {x, rt});
-        TDC_FOR_VEC(vec, T, V, TDC_FOR_ACT(p->shape.act, ACT, {
-            if (y) tdc_norm_apply<T, V, ACT><<<grid, TDC_NORM_THREADS, d.G * sizeof(float2), s>>>(d, xt, xp, gamma, beta, rt, rp, (T *)y, yp, p->partial, a.mean, a.rstd);
-            else tdc_norm_apply_mx4<T, V, ACT><<<grid, TDC_NORM_THREADS, d.G * sizeof(float2), s>>>(d, xt, xp, gamma, beta, rt, rp, codes, scales, p->partial, a.mean, a.rstd);
-        }));
+        TDC_FOR_VEC(V0, T, V, {
+            const size_t lds = d.G * sizeof(float2);
+            if (y) tdc_norm_apply<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
+            else if (!lanes) tdc_norm_apply_blocks<T, V><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
+            else if constexpr (V * sizeof(T) == 16) tdc_norm_apply<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
+        });
     });
     return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }

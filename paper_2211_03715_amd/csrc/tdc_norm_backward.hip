@@ -1,186 +1,382 @@
-// Backward pass of the group norm with an activation (tdc_norm.h), in three kernels:
-//   1. per chunk and channel, sum d and sum d xhat, with d = dy act'(pre) recomputed from x;
-//   2. dgamma and dbeta, sums over all images and chunks; and for every image and group the means of g and g xhat, g = d gamma;
-//   3. dx = rstd (g - m(g) - xhat m(g xhat)), and dresidual = d.
-#include <initializer_list>
-
+// Backward pass of the group norm with an activation (tdc_norm.h).
+//
+// With d = dy act'(pre), recomputed from x, and g = d gamma: dx needs the sums of g and g xhat over a group of an image, dgamma
+// and dbeta those of d xhat and d over all images.  Resident: a workgroup keeps its slice of x and dy in registers, reads them
+// once, and goes through several images with its channels' sums; a second launch adds up what the workgroups have for each
+// channel.  Over chunks: a first kernel leaves the sums of every chunk and group, and its channels' sums; the second combines an
+// image's, runs over the pixels again, and in its last workgroups adds up the channels' sums.
 #include "tdc_norm_internal.h"
 
 namespace {
 
-struct GradPtrs {
+struct GradIn {
+    const void *x, *dy, *residual;
     const float *mean, *rstd, *gamma, *beta;
-    int64_t xp, rp, dyp, dxp, drp;
+    int64_t xp, dyp, rp;
+    int act;
+};
+
+struct GradOut {
+    void *dx, *dresidual;
+    int64_t dxp, drp;
 };
 
 // What a thread needs to know of its V channels.
 template <int V> struct Channels {
     float mean[V], rstd[V], gamma[V], beta[V];
-    __device__ __forceinline__ Channels(const TdcNormDims &d, const GradPtrs &q, int b, int c0)
+    __device__ __forceinline__ void weights(const GradIn &q, int c0)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            gamma[v] = q.gamma ? q.gamma[c0 + v] : 1.f;
+            beta[v] = q.beta ? q.beta[c0 + v] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void statistics(const TdcNormDims &d, const GradIn &q, int b, int c0)
     {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const size_t g = (size_t)b * d.G + (c0 + v) / d.Cg;
             mean[v] = q.mean[g];
             rstd[v] = q.rstd[g];
-            gamma[v] = q.gamma ? q.gamma[c0 + v] : 1.f;
-            beta[v] = q.beta ? q.beta[c0 + v] : 0.f;
         }
     }
 };
 
 // d and xhat of V channels of a pixel.  pre is computed as the forward kernel does, so that both see the same side of a ReLU.
-template <typename T, int V, int ACT>
-__device__ __forceinline__ void tdc_norm_d(const Channels<V> &k, const TdcVec<T, V> &x, const TdcVec<T, V> &dy, const TdcVec<T, V> &res, bool has_res,
-                                           float (&dd)[V], float (&xhat)[V])
+template <typename T, int V>
+__device__ __forceinline__ void gradient(const Channels<V> &k, const TdcVec<T, V> &x, const TdcVec<T, V> &dy, const TdcVec<T, V> &res, const GradIn &q, float (&dd)[V],
+                                         float (&xhat)[V])
 {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float off = (float)x.v[v] - k.mean[v];
-        xhat[v] = off * k.rstd[v];
+        xhat[v] = ((float)x.v[v] - k.mean[v]) * k.rstd[v];
         dd[v] = (float)dy.v[v];
-        if (ACT != TDC_ACT_NONE) {
-            float pre = off * (k.rstd[v] * k.gamma[v]) + k.beta[v];
-            if (has_res) pre += (float)res.v[v];
-            dd[v] *= tdc_activate_grad<ACT>(pre);
+    }
+    if (q.act != TDC_ACT_NONE) {
+        float pre[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) pre[v] = ((float)x.v[v] - k.mean[v]) * (k.rstd[v] * k.gamma[v]) + k.beta[v];
+        if (q.residual) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) pre[v] += (float)res.v[v];
         }
+#pragma unroll
+        for (int v = 0; v < V; ++v) dd[v] *= q.act == TDC_ACT_RELU ? tdc_activate_grad<TDC_ACT_RELU>(pre[v]) : tdc_activate_grad<TDC_ACT_SILU>(pre[v]);
     }
 }
 
-template <typename T, int V, int ACT>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDims d, GradPtrs q, const T *__restrict__ x, const T *__restrict__ dy,
-                                                                        const T *__restrict__ res, float2 *__restrict__ partial)
+template <typename T, int V>
+__device__ __forceinline__ void store_gradients(const Channels<V> &k, const GradOut &out, const float (&m1)[V], const float (&m2)[V], const float (&dd)[V], const float (&xhat)[V], size_t px, int c0)
 {
-    extern __shared__ float2 chan[];                       // [rows][C]
-    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x;
-    const int len = tdc_chunk_len(d, chunk);
-    const int rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-    const int r = rows == 1 ? 0 : threadIdx.x / nv;
-    const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
-    float2 *out = partial + ((size_t)b * d.chunks + chunk) * d.C;
-    if (r < rows)
-        for (int cv = rows == 1 ? threadIdx.x : threadIdx.x - r * nv; cv < nv; cv += TDC_NORM_THREADS) {
-            const Channels<V> k(d, q, b, cv * V);
+    float o[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) o[v] = k.rstd[v] * (dd[v] * k.gamma[v] - m1[v] - xhat[v] * m2[v]);
+    tdc_store<T, V>(static_cast<T *>(out.dx) + px * out.dxp + c0, o);
+    if (out.dresidual) tdc_store<T, V>(static_cast<T *>(out.dresidual) + px * out.drp + c0, dd);
+}
+
+// A thread's channels' sums as items of groups: with their weights, the piece as a whole (WHOLE) or every channel by itself.
+template <int V, bool WHOLE> __device__ __forceinline__ void put_items(float2 *items, int row, int nv, int cv, const Channels<V> &k, const float (&s1)[V], const float (&s2)[V])
+{
+    if constexpr (WHOLE) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            a += s1[v] * k.gamma[v];
+            b += s2[v] * k.gamma[v];
+        }
+        items[row * nv + cv] = make_float2(a, b);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) items[(row * nv + cv) * V + v] = make_float2(s1[v] * k.gamma[v], s2[v] * k.gamma[v]);
+    }
+}
+
+// Channels' sums of the workgroup's rows, [rows][width] in LDS, added up into `out` [width]: some threads to a channel first.
+__device__ __forceinline__ void add_rows(float2 *chan, int rows, int width, float2 *out, int threads)
+{
+    const int per = max(1, min(threads / width, rows));
+    __syncthreads();
+    const int c = threadIdx.x % width, k = threadIdx.x / width;
+    if (per > 1) {
+        float s1 = 0.f, s2 = 0.f;
+        if (k < per)
+            for (int i = k; i < rows; i += per) {
+                s1 += chan[i * width + c].x;
+                s2 += chan[i * width + c].y;
+            }
+        __syncthreads();
+        if (k < per) chan[k * width + c] = make_float2(s1, s2);
+        __syncthreads();
+        rows = per;
+    }
+    for (int i = threadIdx.x; i < width; i += threads) {
+        float s1 = 0.f, s2 = 0.f;
+        for (int j = 0; j < rows; ++j) {
+            s1 += chan[j * width + i].x;
+            s2 += chan[j * width + i].y;
+        }
+        out[i] = make_float2(s1, s2);
+    }
+}
+
+// dgamma and dbeta of 32 channels from `rows` rows of channels' sums, THREADS / 32 threads to a channel.
+template <int THREADS> __device__ __forceinline__ void add_weights(int C, const float2 *sums, int rows, int c0, float *dgamma, float *dbeta)
+{
+    __shared__ float2 tot[THREADS];
+    const int c = c0 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+    float s1 = 0.f, s2 = 0.f;
+    if (c < C) {
+#pragma unroll 4
+        for (int i = k; i < rows; i += THREADS / 32) {
+            const float2 v = sums[(size_t)i * C + c];
+            s1 += v.x;
+            s2 += v.y;
+        }
+    }
+    tot[threadIdx.x] = make_float2(s1, s2);
+    __syncthreads();
+    if (k == 0 && c < C) {
+        for (int i = 1; i < THREADS / 32; ++i) {
+            s1 += tot[32 * i + threadIdx.x].x;
+            s2 += tot[32 * i + threadIdx.x].y;
+        }
+        if (dgamma) dgamma[c] = s2;
+        if (dbeta) dbeta[c] = s1;
+    }
+}
+
+template <int THREADS> __global__ __launch_bounds__(THREADS) void tdc_norm_grad_weights(int C, const float2 *__restrict__ sums, int rows, float *__restrict__ dgamma, float *__restrict__ dbeta)
+{
+    add_weights<THREADS>(C, sums, rows, blockIdx.x * 32, dgamma, dbeta);
+}
+
+// ---- resident: workgroup (row, slice) takes images row, row + rows_of_images, ...
+template <typename T, int V, bool WHOLE, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d, GradIn q, GradOut out, int width, int slices, float2 *__restrict__ sums)
+{
+    __shared__ float2 items[THREADS * V], means[THREADS];
+    int image, slice;
+    tdc_norm_place(blockIdx.x, gridDim.x, slices, image, slice);
+    const int first = image, images = gridDim.x / slices, nv = width / V, groups = width / d.Cg;
+    const TdcNormLanes t(nv, THREADS);
+    const bool live = t.r < min(t.rows, d.P) && t.cv < nv;
+    const int c0 = slice * width + (live ? t.cv * V : 0), g0 = slice * width / d.Cg;
+    const float inv = 1.f / ((float)d.P * d.Cg);
+    Channels<V> k;
+    k.weights(q, c0);
+    float t1[V], t2[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) t1[v] = t2[v] = 0.f;
+    for (; image < d.B; image += images) {
+        const size_t first_px = (size_t)image * d.P;
+        TdcVec<T, V> x[HELD], dy[HELD];
+        const T *res = static_cast<const T *>(q.residual);
+        const bool has_res = res && q.act != TDC_ACT_NONE;
+        k.statistics(d, q, image, c0);
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const size_t px = first_px + tdc_anew(min(t.r + i * t.rows, d.P - 1));
+                x[i] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + c0);
+                dy[i] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + c0);
+            }
             float s1[V], s2[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
-            for (int p = r; p < len; p += rows) {
-                const size_t px = first + p;
-                const TdcVec<T, V> xv = tdc_load<T, V>(x + px * q.xp + cv * V), dv = tdc_load<T, V>(dy + px * q.dyp + cv * V);
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int p = tdc_anew(t.r + i * t.rows);
+                if (p >= d.P) break;
                 TdcVec<T, V> rv;
-                if (ACT != TDC_ACT_NONE && res) rv = tdc_load<T, V>(res + px * q.rp + cv * V);
+                if (has_res) rv = tdc_load<T, V>(res + (first_px + p) * q.rp + c0);
                 float dd[V], xhat[V];
-                tdc_norm_d<T, V, ACT>(k, xv, dv, rv, res != nullptr, dd, xhat);
+                gradient(k, x[i], dy[i], rv, q, dd, xhat);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     s1[v] += dd[v];
                     s2[v] += dd[v] * xhat[v];
                 }
             }
+            put_items<V, WHOLE>(items, t.r, nv, t.cv, k, s1, s2);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (rows == 1) out[cv * V + v] = make_float2(s1[v], s2[v]);
-                else chan[r * d.C + cv * V + v] = make_float2(s1[v], s2[v]);
+                t1[v] += s1[v];
+                t2[v] += s2[v];
             }
-            if (rows > 1) break;
         }
-    if (rows == 1) return;
-    __syncthreads();
-    for (int c = threadIdx.x; c < d.C; c += TDC_NORM_THREADS) {
-        float s1 = 0.f, s2 = 0.f;
-        for (int i = 0; i < rows; ++i) {
-            s1 += chan[i * d.C + c].x;
-            s2 += chan[i * d.C + c].y;
+        __syncthreads();
+        tdc_norm_group_sums(items, min(t.rows, d.P), groups, WHOLE ? d.Cg / V : d.Cg, THREADS, [&](int g, float a, float b) { means[g] = make_float2(a * inv, b * inv); });
+        __syncthreads();
+        if (live) {
+            float m1[V], m2[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float2 m = means[(c0 + v) / d.Cg - g0];
+                m1[v] = m.x;
+                m2[v] = m.y;
+            }
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int p = tdc_anew(t.r + i * t.rows);
+                if (p >= d.P) break;
+                tdc_forget(x[i]);
+                tdc_forget(dy[i]);
+                TdcVec<T, V> rv;
+                if (has_res) rv = tdc_load<T, V>(res + (first_px + p) * q.rp + c0);
+                float dd[V], xhat[V];
+                gradient(k, x[i], dy[i], rv, q, dd, xhat);
+                store_gradients<T, V>(k, out, m1, m2, dd, xhat, first_px + p, c0);
+            }
         }
-        out[c] = make_float2(s1, s2);
     }
+    if (!sums) return;
+    __syncthreads();
+    if (live) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) items[(t.r * nv + t.cv) * V + v] = make_float2(t1[v], t2[v]);
+    }
+    add_rows(items, min(t.rows, d.P), width, sums + (size_t)first * d.C + slice * width, THREADS);
 }
 
-// Workgroups 0 .. weight_blocks-1: dgamma and dbeta of 32 channels, eight threads to a channel.  The others: an image each.
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_reduce(TdcNormDims d, const float *__restrict__ gamma, const float2 *__restrict__ partial,
-                                                                          int weight_blocks, float *__restrict__ dgamma, float *__restrict__ dbeta, float2 *__restrict__ means)
+// ---- sums of chunks: grid (chunks, rows of images)
+template <typename T, int V, bool WHOLE>
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDims d, GradIn q, float2 *__restrict__ partial, float2 *__restrict__ sums)
 {
-    extern __shared__ float2 tot[];                        // [C], or [8][32]
-    if ((int)blockIdx.x < weight_blocks) {
-        const int c = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
-        float s1 = 0.f, s2 = 0.f;
-        if (c < d.C)
-            for (size_t i = lane; i < (size_t)d.B * d.chunks; i += 8) {
-                const float2 v = partial[i * d.C + c];
-                s1 += v.x;
-                s2 += v.y;
+    constexpr int U = TDC_NORM_UNROLL / 2;
+    extern __shared__ float2 items[];                      // rows * C, twice where a pixel takes several sweeps
+    const int nv = d.C / V, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
+    const TdcNormLanes t(nv, TDC_NORM_THREADS);
+    const int used = min(t.rows, len);
+    const T *res = q.act != TDC_ACT_NONE ? static_cast<const T *>(q.residual) : nullptr;
+    float t1[V], t2[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) t1[v] = t2[v] = 0.f;
+    for (int b = blockIdx.y; b < d.B; b += gridDim.y) {
+        const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
+        if (t.r < used)
+            for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
+                Channels<V> k;
+                k.weights(q, cv * V);
+                k.statistics(d, q, b, cv * V);
+                float s1[V], s2[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
+                for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
+                    TdcVec<T, V> xv[U], dv[U], rv[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const size_t px = first + min(p0 + u * t.rows, len - 1);
+                        xv[u] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + cv * V);
+                        dv[u] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
+                        if (res) rv[u] = tdc_load<T, V>(res + px * q.rp + cv * V);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (p0 + u * t.rows >= len) break;
+                        float dd[V], xhat[V];
+                        gradient(k, xv[u], dv[u], rv[u], q, dd, xhat);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            s1[v] += dd[v];
+                            s2[v] += dd[v] * xhat[v];
+                        }
+                    }
+                }
+                put_items<V, WHOLE>(items, t.r, nv, cv, k, s1, s2);
+                if (t.rows > 1 || nv <= TDC_NORM_THREADS) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        t1[v] += s1[v];
+                        t2[v] += s2[v];
+                    }
+                } else if (sums) {
+                    // several sweeps to a pixel: the channels' sums of this workgroup, which no other touches, stay in its row
+                    float2 *row = sums + (size_t)(blockIdx.y * gridDim.x + chunk) * d.C + cv * V;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float2 o = b == (int)blockIdx.y ? make_float2(0.f, 0.f) : row[v];
+                        row[v] = make_float2(o.x + s1[v], o.y + s2[v]);
+                    }
+                }
+                if (t.rows > 1) break;
             }
-        tot[threadIdx.x] = make_float2(s1, s2);
         __syncthreads();
-        if (lane == 0 && c < d.C) {
-            for (int i = 1; i < 8; ++i) {
-                s1 += tot[32 * i + threadIdx.x].x;
-                s2 += tot[32 * i + threadIdx.x].y;
-            }
-            if (dgamma) dgamma[c] = s2;
-            if (dbeta) dbeta[c] = s1;
-        }
+        float2 *to = partial + ((size_t)b * d.chunks + chunk) * d.G;
+        tdc_norm_group_sums(items, used, d.G, WHOLE ? d.Cg / V : d.Cg, TDC_NORM_THREADS, [&](int g, float s1, float s2) { to[g] = make_float2(s1, s2); });
+        __syncthreads();
+    }
+    if (!sums || nv > TDC_NORM_THREADS) return;
+    if (t.r < used && t.cv < nv) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) items[(t.r * nv + t.cv) * V + v] = make_float2(t1[v], t2[v]);
+    }
+    add_rows(items, used, d.C, sums + (size_t)(blockIdx.y * gridDim.x + chunk) * d.C, TDC_NORM_THREADS);
+}
+
+// ---- gradients of chunks: grid (chunks, batch), and behind them the workgroups that add up the channels' sums
+template <typename T, int V>
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormDims d, GradIn q, GradOut out, const float2 *__restrict__ partial, const float2 *__restrict__ sums, int rows,
+                                                                         float *__restrict__ dgamma, float *__restrict__ dbeta)
+{
+    constexpr int U = TDC_NORM_UNROLL / 2;
+    extern __shared__ float2 means[];                      // [G]
+    const int id = blockIdx.x, b = id / d.chunks, chunk = id - b * d.chunks;
+    if (b >= d.B) {
+        add_weights<TDC_NORM_THREADS>(d.C, sums, rows, (id - d.B * d.chunks) * 32, dgamma, dbeta);
         return;
     }
-    const int b = blockIdx.x - weight_blocks;
-    for (int c = threadIdx.x; c < d.C; c += TDC_NORM_THREADS) {
-        const float2 *p = partial + (size_t)b * d.chunks * d.C + c;
-        float s1 = 0.f, s2 = 0.f;
-        for (int i = 0; i < d.chunks; ++i) {
-            s1 += p[(size_t)i * d.C].x;
-            s2 += p[(size_t)i * d.C].y;
-        }
-        const float w = gamma ? gamma[c] : 1.f;
-        tot[c] = make_float2(s1 * w, s2 * w);
-    }
-    __syncthreads();
-    const int L = tdc_team(d.G, d.Cg), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = TDC_NORM_THREADS / L;
+    const int nv = d.C / V, len = tdc_chunk_len(d, chunk);
+    const int L = tdc_team(d.G, d.chunks, TDC_NORM_THREADS), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = TDC_NORM_THREADS / L;
     const float inv = 1.f / ((float)d.P * d.Cg);
     for (int g0 = 0; g0 < d.G; g0 += teams) {
         const int g = min(g0 + team, d.G - 1);
+        const float2 *p = partial + (size_t)b * d.chunks * d.G + g;
         float s1 = 0.f, s2 = 0.f;
-        for (int c = lane; c < d.Cg; c += L) {
-            s1 += tot[g * d.Cg + c].x;
-            s2 += tot[g * d.Cg + c].y;
+        for (int i = lane; i < d.chunks; i += L) {
+            const float2 o = p[(size_t)i * d.G];
+            s1 += o.x;
+            s2 += o.y;
         }
         s1 = tdc_lane_sum(s1, L);
         s2 = tdc_lane_sum(s2, L);
-        if (lane == 0 && g0 + team < d.G) means[(size_t)b * d.G + g] = make_float2(s1 * inv, s2 * inv);
+        if (lane == 0 && g0 + team < d.G) means[g] = make_float2(s1 * inv, s2 * inv);
     }
-}
-
-template <typename T, int V, int ACT>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormDims d, GradPtrs q, const T *__restrict__ x, const T *__restrict__ dy,
-                                                                         const T *__restrict__ res, const float2 *__restrict__ means, T *__restrict__ dx, T *__restrict__ dres)
-{
-    const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x;
-    const int len = tdc_chunk_len(d, chunk);
-    const int rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-    const int r = rows == 1 ? 0 : threadIdx.x / nv;
-    if (r >= rows) return;
+    __syncthreads();
+    const TdcNormLanes t(nv, TDC_NORM_THREADS);
+    if (t.r >= t.rows) return;
     const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
-    for (int cv = rows == 1 ? threadIdx.x : threadIdx.x - r * nv; cv < nv; cv += TDC_NORM_THREADS) {
-        const Channels<V> k(d, q, b, cv * V);
+    const T *res = q.act != TDC_ACT_NONE ? static_cast<const T *>(q.residual) : nullptr;
+    for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
+        Channels<V> k;
+        k.weights(q, cv * V);
+        k.statistics(d, q, b, cv * V);
         float m1[V], m2[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float2 m = means[(size_t)b * d.G + (cv * V + v) / d.Cg];
+            const float2 m = means[(cv * V + v) / d.Cg];
             m1[v] = m.x;
             m2[v] = m.y;
         }
-        for (int p = r; p < len; p += rows) {
-            const size_t px = first + p;
-            const TdcVec<T, V> xv = tdc_load<T, V>(x + px * q.xp + cv * V), dv = tdc_load<T, V>(dy + px * q.dyp + cv * V);
-            TdcVec<T, V> rv;
-            if (ACT != TDC_ACT_NONE && res) rv = tdc_load<T, V>(res + px * q.rp + cv * V);
-            float dd[V], xhat[V], o[V];
-            tdc_norm_d<T, V, ACT>(k, xv, dv, rv, res != nullptr, dd, xhat);
+        for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
+            TdcVec<T, V> xv[U], dv[U], rv[U];
 #pragma unroll
-            for (int v = 0; v < V; ++v) o[v] = k.rstd[v] * (dd[v] * k.gamma[v] - m1[v] - xhat[v] * m2[v]);
-            tdc_store<T, V>(dx + px * q.dxp + cv * V, o);
-            if (dres) tdc_store<T, V>(dres + px * q.drp + cv * V, dd);
+            for (int u = 0; u < U; ++u) {
+                const size_t px = first + min(p0 + u * t.rows, len - 1);
+                xv[u] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + cv * V);
+                dv[u] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
+                if (res) rv[u] = tdc_load<T, V>(res + px * q.rp + cv * V);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (p0 + u * t.rows >= len) break;
+                float dd[V], xhat[V];
+                gradient(k, xv[u], dv[u], rv[u], q, dd, xhat);
+                store_gradients<T, V>(k, out, m1, m2, dd, xhat, first + p0 + u * t.rows, cv * V);
+            }
         }
-        if (rows > 1) break;
+        if (t.rows > 1) break;
     }
 }
 
@@ -195,25 +391,39 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
     const TdcNormDims &d = p->dims;
     const int dt = p->shape.dtype, size = tdc_dtype_bytes(dt);
     auto pitch = [&](int64_t v) { return v ? v : (int64_t)d.C; };
-    const GradPtrs q{mean, rstd, gamma, beta, pitch(a.x_pitch), pitch(a.residual_pitch), pitch(a.dy_pitch), pitch(a.dx_pitch), pitch(a.dresidual_pitch)};
-    for (int64_t v : {q.xp, q.rp, q.dyp, q.dxp, q.drp})
+    const GradIn q{x, dy, a.residual, mean, rstd, gamma, beta, pitch(a.x_pitch), pitch(a.dy_pitch), pitch(a.residual_pitch), p->shape.act};
+    const GradOut out{dx, a.dresidual, pitch(a.dx_pitch), pitch(a.dresidual_pitch)};
+    for (int64_t v : {q.xp, q.rp, q.dyp, out.dxp, out.drp})
         if (v < d.C) return TDC_ERR_BAD_SHAPE;
     for (const void *v : {x, dy, a.residual, (const void *)dx, (const void *)a.dresidual})
         if (!tdc_aligned_to(v, size)) return TDC_ERR_UNSUPPORTED;
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
     hipStream_t s = (hipStream_t)hip_stream;
-    const dim3 grid(d.chunks, d.B);
     const int weight_blocks = dgamma || dbeta ? (d.C + 31) / 32 : 0;
-    const int vec = tdc_norm_vec(dt, d.C, {q.xp, a.residual ? q.rp : 0, q.dyp, q.dxp, a.dresidual ? q.drp : 0}, {x, dy, a.residual, dx, a.dresidual});
-    TDC_FOR_DTYPE(dt, T, {
-        const T *xt = (const T *)x, *dyt = (const T *)dy, *rt = (const T *)a.residual;
-        TDC_FOR_VEC(vec, T, V, TDC_FOR_ACT(p->shape.act, ACT, {
-            const int nv = d.C / V, rows = nv <= TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
-            tdc_norm_grad_sums<T, V, ACT><<<grid, TDC_NORM_THREADS, rows == 1 ? 0 : (size_t)rows * d.C * sizeof(float2), s>>>(d, q, xt, dyt, rt, p->partial);
-            tdc_norm_grad_reduce<<<weight_blocks + d.B, TDC_NORM_THREADS, std::max(d.C, TDC_NORM_THREADS) * sizeof(float2), s>>>(d, gamma, p->partial, weight_blocks, dgamma, dbeta, p->means);
-            tdc_norm_grad_apply<T, V, ACT><<<grid, TDC_NORM_THREADS, 0, s>>>(d, q, xt, dyt, rt, p->means, (T *)dx, (T *)a.dresidual);
-        }));
-    });
+    float2 *sums = weight_blocks ? p->sums : nullptr;
+    const int vec = tdc_norm_vec(dt, d.C, {q.xp, a.residual ? q.rp : 0, q.dyp, out.dxp, a.dresidual ? out.drp : 0}, {x, dy, a.residual, dx, a.dresidual}, 4);
+    const bool whole = d.Cg % vec == 0;
+    const TdcNormSlice sl = tdc_norm_slice(d, dt, vec, true, 1);
+    if (sl.held) {
+        const int rows = std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / sl.slices));
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), true), THREADS, HELD, {
+            const unsigned wgs = (unsigned)rows * sl.slices;
+            if (whole) tdc_norm_grad_resident<T, V, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sums);
+            else tdc_norm_grad_resident<T, V, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sums);
+        })));
+        if (sums) tdc_norm_grad_weights<256><<<weight_blocks, 256, 0, s>>>(d.C, sums, rows, dgamma, dbeta);
+        return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    }
+    const int images = std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / d.chunks));
+    float2 *partial = reinterpret_cast<float2 *>(p->partial);
+    TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, {
+        const int nv = d.C / V, rows = nv < TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
+        const size_t lds = (size_t)rows * d.C * sizeof(float2);
+        const dim3 grid(d.chunks, images);
+        if (whole) tdc_norm_grad_sums<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
+        else tdc_norm_grad_sums<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
+        tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks + weight_blocks, TDC_NORM_THREADS, d.G * sizeof(float2), s>>>(d, q, out, partial, sums, images * d.chunks, dgamma, dbeta);
+    }));
     return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }

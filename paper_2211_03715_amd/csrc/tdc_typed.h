@@ -27,6 +27,26 @@ template <typename T, int V> __device__ __forceinline__ TdcVec<T, V> tdc_load(co
     return *reinterpret_cast<const TdcVec<T, V> *>(p);
 }
 
+// Makes the compiler take `x` for something new, so that what it computed from x before is computed again and not kept: a
+// kernel that goes twice over pieces in registers has no room for both the pieces and their values.
+template <typename T, int V> __device__ __forceinline__ void tdc_forget(TdcVec<T, V> &x)
+{
+    if constexpr (sizeof(T) * V >= 4) {
+        unsigned w[sizeof(T) * V / 4];
+        __builtin_memcpy(w, &x, sizeof(w));
+#pragma unroll
+        for (unsigned &u : w) asm volatile("" : "+v"(u));
+        __builtin_memcpy(&x, w, sizeof(w));
+    }
+}
+
+// The same for an index, whose addresses are then made where they are used and do not fill registers until then.
+__device__ __forceinline__ int tdc_anew(int i)
+{
+    asm volatile("" : "+v"(i));
+    return i;
+}
+
 template <typename T, int V> __device__ __forceinline__ void tdc_store(T *p, const float (&f)[V])
 {
     TdcVec<T, V> o;
@@ -43,6 +63,17 @@ template <int ACT> __device__ __forceinline__ float tdc_activate(float v)
     if constexpr (ACT == TDC_ACT_RELU) return v > 0.f ? v : (v != v ? v : 0.f);   // a NaN stays one
     if constexpr (ACT == TDC_ACT_SILU) return v * tdc_sigmoid(v);
     return v;
+}
+
+template <int V> __device__ __forceinline__ void tdc_activate_all(int act, float (&v)[V])
+{
+    if (act == TDC_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = tdc_activate<TDC_ACT_RELU>(v[i]);
+    } else if (act == TDC_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = tdc_activate<TDC_ACT_SILU>(v[i]);
+    }
 }
 
 // act'(v)
@@ -81,6 +112,13 @@ __device__ __forceinline__ float tdc_lane_sum(float v, int lanes)
     do {                                                                                  \
         if ((v) == 8) { if constexpr (sizeof(T) == 2) { constexpr int V = 8; __VA_ARGS__; } } \
         else if ((v) == 4) { constexpr int V = 4; __VA_ARGS__; }                          \
+        else if ((v) == 2) { constexpr int V = 2; __VA_ARGS__; }                          \
+        else { constexpr int V = 1; __VA_ARGS__; }                                        \
+    } while (0)
+
+#define TDC_FOR_VEC4(v, V, ...)                                                           \
+    do {                                                                                  \
+        if ((v) == 4) { constexpr int V = 4; __VA_ARGS__; }                               \
         else if ((v) == 2) { constexpr int V = 2; __VA_ARGS__; }                          \
         else { constexpr int V = 1; __VA_ARGS__; }                                        \
     } while (0)
