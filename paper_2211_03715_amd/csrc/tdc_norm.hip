@@ -28,13 +28,12 @@ template <int V> struct Affine {
     // stats: of the groups from g0 on
     __device__ __forceinline__ void set(const TdcNormDims &d, const NormIn &in, const float2 *stats, int g0, int c0)
     {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float2 st = stats[(c0 + v) / d.Cg - g0];
+        tdc_norm_channels<V>(c0, d.Cg, [&](int v, int g) {
+            const float2 st = stats[g - g0];
             mean[v] = st.x;
             scale[v] = in.gamma ? st.y * in.gamma[c0 + v] : st.y;
             shift[v] = in.beta ? in.beta[c0 + v] : 0.f;
-        }
+        });
     }
 };
 
@@ -56,9 +55,7 @@ template <int V> __device__ __forceinline__ void store_mx4(const NormOut &out, c
     unsigned top = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) top = max(top, tdc_abs_bits(o[v]));
-#pragma unroll
-    for (int l = 1; l < 32 / V; l <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, l, 64));
-    const unsigned e = tdc_mx4_scale(top);
+    const unsigned e = tdc_mx4_scale(tdc_lane_max<32 / V>(top));
     if (!live) return;
     const size_t block = px * nb + c0 / 32;
     uint8_t *at = out.codes + block * 16 + (c0 % 32) / 2;
@@ -69,27 +66,30 @@ template <int V> __device__ __forceinline__ void store_mx4(const NormOut &out, c
 
 // ---- resident: a slice of an image's channels in the registers of a workgroup
 template <typename T, int V, bool WHOLE, bool MX4, int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS) void tdc_norm_resident(TdcNormDims d, NormIn in, NormOut out, int width, int slices)
+__global__ __launch_bounds__(THREADS) void tdc_norm_resident(TdcNormDims d, NormIn in, NormOut out, int width, int slices, int held_here)
 {
-    __shared__ float2 items[THREADS * (WHOLE ? 1 : V)], stats[THREADS];
+    __shared__ float2 item[THREADS * (WHOLE ? 1 : V)], stats[THREADS];
+    __shared__ float count[THREADS];
+    const TdcNormItems items{item, count};
     int b, slice;
     tdc_norm_place(blockIdx.x, gridDim.x, slices, b, slice);
     const int nv = width / V, groups = width / d.Cg, c0 = slice * width;
     const TdcNormLanes t(nv, THREADS);
-    const bool live = t.r < t.rows && t.cv < nv;
+    const bool live = t.r < min(t.rows, d.P) && t.cv < nv;
     const T *x = static_cast<const T *>(in.x) + (size_t)b * d.P * in.xp + c0 + t.cv * V;
     TdcVec<T, V> held[HELD];
-    const int k = live && t.r < d.P ? (d.P - t.r + t.rows - 1) / t.rows : 0;   // pixels of this thread
-    if (k) {
+    TdcNormSums<V, WHOLE> sums;
+    if (live) {
+        // held_here is the same for all threads: what lies behind it is skipped without a load
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) held[i] = tdc_load<T, V>(x + (size_t)min(t.r + i * t.rows, d.P - 1) * in.xp);
-        TdcNormSums<V> sums;
-        sums.add(held, k);
-        sums.template put<WHOLE>(items, t.r, nv, t.cv);
+        for (int i = 0; i < HELD; ++i)
+            if (i < held_here) held[i] = tdc_load<T, V>(x + (size_t)min(t.r + i * t.rows, d.P - 1) * in.xp);
+        sums.add(held, (d.P - t.r + t.rows - 1) / t.rows);
     }
+    const int rows = tdc_norm_put<V, WHOLE, THREADS>(items, sums, t, t.cv, nv, live, min(t.rows, d.P));
     __syncthreads();
     const size_t at = (size_t)b * d.G + c0 / d.Cg;
-    tdc_norm_groups(items, min(t.rows, d.P), d.P / t.rows, d.P % t.rows, groups, WHOLE ? d.Cg / V : d.Cg, WHOLE ? V : 1, THREADS, [&](int g, float n, float mean, float m2) {
+    tdc_norm_groups<THREADS>(items, rows, groups, WHOLE ? d.Cg / V : d.Cg, [&](int g, float n, float mean, float m2) {
         const float rstd = tdc_rstd(m2 / n, d.eps);
         stats[g] = make_float2(mean, rstd);
         if (out.mean) out.mean[at + g] = mean;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(THREADS) void tdc_norm_resident(TdcNormDims d, Norm
     for (int i = 0; i < HELD; ++i) {
         const int p = tdc_anew(t.r + i * t.rows);
         const bool mine = live && p < d.P;
-        if (!mine && !MX4) break;
+        if (MX4 ? i >= held_here : !mine) break;
         tdc_forget(held[i]);
         TdcVec<T, V> rv;
         if (res && mine) rv = tdc_load<T, V>(res + (size_t)p * in.rp);
@@ -122,26 +122,30 @@ template <typename T, int V, bool WHOLE>
 __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_stats(TdcNormDims d, NormIn in, float4 *__restrict__ partial)
 {
     constexpr int U = TDC_NORM_UNROLL;
-    extern __shared__ float2 items[];
+    extern __shared__ float2 item[];
+    __shared__ float count[TDC_NORM_THREADS];
+    const TdcNormItems items{item, count};
     const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
     const TdcNormLanes t(nv, TDC_NORM_THREADS);
     const T *base = static_cast<const T *>(in.x) + ((size_t)b * d.P + (size_t)chunk * d.chunk_px) * in.xp;
-    if (t.r < min(t.rows, len))
-        for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
-            TdcNormSums<V> sums;
+    const int used = min(t.rows, len);
+    int rows = 1;
+    for (int cv = t.cv; cv < nv || cv == t.cv; cv += TDC_NORM_THREADS) {   // once, but for pixels of more pieces than there are threads
+        const bool live = t.r < used && cv < nv;
+        TdcNormSums<V, WHOLE> sums;
+        if (live)
             for (int p = t.r; p < len; p += t.rows * U) {
                 TdcVec<T, V> v[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(base + (size_t)min(p + u * t.rows, len - 1) * in.xp + cv * V);
                 sums.add(v, min(U, (len - p + t.rows - 1) / t.rows));
             }
-            sums.template put<WHOLE>(items, t.r, nv, cv);
-            if (t.rows > 1) break;
-        }
+        rows = tdc_norm_put<V, WHOLE, TDC_NORM_THREADS>(items, sums, t, cv, nv, live, used);
+        if (t.rows > 1) break;
+    }
     __syncthreads();
     float4 *out = partial + ((size_t)b * d.chunks + chunk) * d.G;
-    tdc_norm_groups(items, min(t.rows, len), len / t.rows, len % t.rows, d.G, WHOLE ? d.Cg / V : d.Cg, WHOLE ? V : 1, TDC_NORM_THREADS,
-                    [&](int g, float n, float mean, float m2) { out[g] = make_float4(n, mean, m2, 0.f); });
+    tdc_norm_groups<TDC_NORM_THREADS>(items, rows, d.G, WHOLE ? d.Cg / V : d.Cg, [&](int g, float n, float mean, float m2) { out[g] = make_float4(n, mean, m2, 0.f); });
 }
 
 // ---- y = act((x - mean) * (rstd gamma) + beta + residual): grid (chunks, batch)
@@ -325,16 +329,16 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);
     if (sl.held) {
-        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC(V0, T, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), false), THREADS, HELD, {
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC(V0, T, V, TDC_FOR_SLICE(sl, 1024, tdc_norm_held(V, sizeof(T), false), THREADS, HELD, {
             const unsigned wgs = (unsigned)d.B * sl.slices;
             if (lanes) {
                 if constexpr (V * sizeof(T) == 16) {
-                    if (whole) tdc_norm_resident<T, V, true, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
-                    else tdc_norm_resident<T, V, false, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+                    if (whole) tdc_norm_resident<T, V, true, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices, sl.held);
+                    else tdc_norm_resident<T, V, false, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices, sl.held);
                 }
             } else {
-                if (whole) tdc_norm_resident<T, V, true, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
-                else tdc_norm_resident<T, V, false, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices);
+                if (whole) tdc_norm_resident<T, V, true, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices, sl.held);
+                else tdc_norm_resident<T, V, false, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, in, out, sl.width, sl.slices, sl.held);
             }
         })));
         return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;

@@ -34,12 +34,10 @@ template <int V> struct Channels {
     }
     __device__ __forceinline__ void statistics(const TdcNormDims &d, const GradIn &q, int b, int c0)
     {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const size_t g = (size_t)b * d.G + (c0 + v) / d.Cg;
-            mean[v] = q.mean[g];
-            rstd[v] = q.rstd[g];
-        }
+        tdc_norm_channels<V>(c0, d.Cg, [&](int v, int g) {
+            mean[v] = q.mean[(size_t)b * d.G + g];
+            rstd[v] = q.rstd[(size_t)b * d.G + g];
+        });
     }
 };
 
@@ -76,30 +74,38 @@ __device__ __forceinline__ void store_gradients(const Channels<V> &k, const Grad
     if (out.dresidual) tdc_store<T, V>(static_cast<T *>(out.dresidual) + px * out.drp + c0, dd);
 }
 
-// A thread's channels' sums as items of groups: with their weights, the piece as a whole (WHOLE) or every channel by itself.
-template <int V, bool WHOLE> __device__ __forceinline__ void put_items(float2 *items, int row, int nv, int cv, const Channels<V> &k, const float (&s1)[V], const float (&s2)[V])
+// A thread's channels' sums as items of groups, into LDS: with their weights, the piece as a whole (WHOLE) or every channel by
+// itself.  Returns the number of rows of items.
+template <int V, bool WHOLE, int THREADS>
+__device__ __forceinline__ int put_items(float2 *items, const TdcNormLanes &t, int cv, int nv, bool live, int used, const Channels<V> &k, const float (&s1)[V], const float (&s2)[V])
 {
+    constexpr int I = WHOLE ? 1 : V;
+    float a[I], b[I];
     if constexpr (WHOLE) {
-        float a = 0.f, b = 0.f;
+        a[0] = b[0] = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            a += s1[v] * k.gamma[v];
-            b += s2[v] * k.gamma[v];
+            a[0] += s1[v] * k.gamma[v];
+            b[0] += s2[v] * k.gamma[v];
         }
-        items[row * nv + cv] = make_float2(a, b);
     } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) items[(row * nv + cv) * V + v] = make_float2(s1[v] * k.gamma[v], s2[v] * k.gamma[v]);
+        for (int v = 0; v < V; ++v) {
+            a[v] = s1[v] * k.gamma[v];
+            b[v] = s2[v] * k.gamma[v];
+        }
     }
+    return tdc_norm_put_sums<I, THREADS>(items, a, b, t, cv, nv, live, used);
 }
 
-// Channels' sums of the workgroup's rows, [rows][width] in LDS, added up into `out` [width]: some threads to a channel first.
-__device__ __forceinline__ void add_rows(float2 *chan, int rows, int width, float2 *out, int threads)
+// The threads' channels' sums added up over the workgroup into `out` [width], through `chan` in LDS, which every thread has left.
+template <int V, int THREADS> __device__ __forceinline__ void add_rows(float2 *chan, float (&t1)[V], float (&t2)[V], const TdcNormLanes &t, int nv, bool live, int used, float2 *out)
 {
-    const int per = max(1, min(threads / width, rows));
+    int rows = tdc_norm_put_sums<V, THREADS>(chan, t1, t2, t, t.cv, nv, live, used);
     __syncthreads();
-    const int c = threadIdx.x % width, k = threadIdx.x / width;
+    const int width = nv * V, per = max(1, min(THREADS / width, rows));
     if (per > 1) {
+        const int k = threadIdx.x / width, c = threadIdx.x - k * width;
         float s1 = 0.f, s2 = 0.f;
         if (k < per)
             for (int i = k; i < rows; i += per) {
@@ -111,7 +117,7 @@ __device__ __forceinline__ void add_rows(float2 *chan, int rows, int width, floa
         __syncthreads();
         rows = per;
     }
-    for (int i = threadIdx.x; i < width; i += threads) {
+    for (int i = threadIdx.x; i < width; i += THREADS) {
         float s1 = 0.f, s2 = 0.f;
         for (int j = 0; j < rows; ++j) {
             s1 += chan[j * width + i].x;
@@ -153,15 +159,17 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void tdc_norm_grad_
 }
 
 // ---- resident: workgroup (row, slice) takes images row, row + rows_of_images, ...
+// After the sums a thread keeps x and d, in fp32: the residual is read once, the activation's slope computed once.
 template <typename T, int V, bool WHOLE, int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d, GradIn q, GradOut out, int width, int slices, float2 *__restrict__ sums)
+__global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d, GradIn q, GradOut out, int width, int slices, int held_here, float2 *__restrict__ sums)
 {
     __shared__ float2 items[THREADS * V], means[THREADS];
     int image, slice;
     tdc_norm_place(blockIdx.x, gridDim.x, slices, image, slice);
     const int first = image, images = gridDim.x / slices, nv = width / V, groups = width / d.Cg;
     const TdcNormLanes t(nv, THREADS);
-    const bool live = t.r < min(t.rows, d.P) && t.cv < nv;
+    const int used = min(t.rows, d.P);
+    const bool live = t.r < used && t.cv < nv, has_res = q.residual && q.act != TDC_ACT_NONE;
     const int c0 = slice * width + (live ? t.cv * V : 0), g0 = slice * width / d.Cg;
     const float inv = 1.f / ((float)d.P * d.Cg);
     Channels<V> k;
@@ -171,73 +179,65 @@ __global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d,
     for (int v = 0; v < V; ++v) t1[v] = t2[v] = 0.f;
     for (; image < d.B; image += images) {
         const size_t first_px = (size_t)image * d.P;
-        TdcVec<T, V> x[HELD], dy[HELD];
-        const T *res = static_cast<const T *>(q.residual);
-        const bool has_res = res && q.act != TDC_ACT_NONE;
-        k.statistics(d, q, image, c0);
+        const T *px = static_cast<const T *>(q.x) + first_px * q.xp + c0, *pdy = static_cast<const T *>(q.dy) + first_px * q.dyp + c0;
+        const T *pres = has_res ? static_cast<const T *>(q.residual) + first_px * q.rp + c0 : nullptr;
+        TdcVec<T, V> x[HELD];
+        float dd[HELD][V], s1[V], s2[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
         if (live) {
+            TdcVec<T, V> dy[HELD], res[HELD];
 #pragma unroll
-            for (int i = 0; i < HELD; ++i) {
-                const size_t px = first_px + tdc_anew(min(t.r + i * t.rows, d.P - 1));
-                x[i] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + c0);
-                dy[i] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + c0);
-            }
-            float s1[V], s2[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
-#pragma unroll
-            for (int i = 0; i < HELD; ++i) {
-                const int p = tdc_anew(t.r + i * t.rows);
-                if (p >= d.P) break;
-                TdcVec<T, V> rv;
-                if (has_res) rv = tdc_load<T, V>(res + (first_px + p) * q.rp + c0);
-                float dd[V], xhat[V];
-                gradient(k, x[i], dy[i], rv, q, dd, xhat);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    s1[v] += dd[v];
-                    s2[v] += dd[v] * xhat[v];
+            for (int i = 0; i < HELD; ++i)
+                if (i < held_here) {
+                    const int p = tdc_anew(min(t.r + i * t.rows, d.P - 1));
+                    x[i] = tdc_load<T, V>(px + (size_t)p * q.xp);
+                    dy[i] = tdc_load<T, V>(pdy + (size_t)p * q.dyp);
+                    if (has_res) res[i] = tdc_load<T, V>(pres + (size_t)p * q.rp);
                 }
-            }
-            put_items<V, WHOLE>(items, t.r, nv, t.cv, k, s1, s2);
+            k.statistics(d, q, image, c0);
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+                if (t.r + i * t.rows < d.P) {
+                    float xhat[V];
+                    gradient(k, x[i], dy[i], res[i], q, dd[i], xhat);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        s1[v] += dd[i][v];
+                        s2[v] += dd[i][v] * xhat[v];
+                    }
+                }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 t1[v] += s1[v];
                 t2[v] += s2[v];
             }
         }
+        const int rows = put_items<V, WHOLE, THREADS>(items, t, t.cv, nv, live, used, k, s1, s2);
         __syncthreads();
-        tdc_norm_group_sums(items, min(t.rows, d.P), groups, WHOLE ? d.Cg / V : d.Cg, THREADS, [&](int g, float a, float b) { means[g] = make_float2(a * inv, b * inv); });
+        tdc_norm_group_sums(items, rows, groups, WHOLE ? d.Cg / V : d.Cg, THREADS, [&](int g, float a, float b) { means[g] = make_float2(a * inv, b * inv); });
         __syncthreads();
         if (live) {
             float m1[V], m2[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float2 m = means[(c0 + v) / d.Cg - g0];
-                m1[v] = m.x;
-                m2[v] = m.y;
-            }
+            tdc_norm_channels<V>(c0, d.Cg, [&](int v, int g) {
+                m1[v] = means[g - g0].x;
+                m2[v] = means[g - g0].y;
+            });
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
                 const int p = tdc_anew(t.r + i * t.rows);
                 if (p >= d.P) break;
                 tdc_forget(x[i]);
-                tdc_forget(dy[i]);
-                TdcVec<T, V> rv;
-                if (has_res) rv = tdc_load<T, V>(res + (first_px + p) * q.rp + c0);
-                float dd[V], xhat[V];
-                gradient(k, x[i], dy[i], rv, q, dd, xhat);
-                store_gradients<T, V>(k, out, m1, m2, dd, xhat, first_px + p, c0);
+                float xhat[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) xhat[v] = ((float)x[i].v[v] - k.mean[v]) * k.rstd[v];
+                store_gradients<T, V>(k, out, m1, m2, dd[i], xhat, first_px + p, c0);
             }
         }
     }
     if (!sums) return;
     __syncthreads();
-    if (live) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) items[(t.r * nv + t.cv) * V + v] = make_float2(t1[v], t2[v]);
-    }
-    add_rows(items, min(t.rows, d.P), width, sums + (size_t)first * d.C + slice * width, THREADS);
+    add_rows<V, THREADS>(items, t1, t2, t, nv, live, used, sums + (size_t)first * d.C + slice * width);
 }
 
 // ---- sums of chunks: grid (chunks, rows of images)
@@ -255,14 +255,16 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDi
     for (int v = 0; v < V; ++v) t1[v] = t2[v] = 0.f;
     for (int b = blockIdx.y; b < d.B; b += gridDim.y) {
         const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
-        if (t.r < used)
-            for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
-                Channels<V> k;
-                k.weights(q, cv * V);
-                k.statistics(d, q, b, cv * V);
-                float s1[V], s2[V];
+        int rows = 1;
+        for (int cv = t.cv; cv < nv || cv == t.cv; cv += TDC_NORM_THREADS) {   // once, but for pixels of more pieces than there are threads
+            const bool live = t.r < used && cv < nv;
+            Channels<V> k;
+            float s1[V], s2[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
+            for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
+            k.weights(q, live ? cv * V : 0);
+            if (live) {
+                k.statistics(d, q, b, cv * V);
                 for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
                     TdcVec<T, V> xv[U], dv[U], rv[U];
 #pragma unroll
@@ -284,8 +286,7 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDi
                         }
                     }
                 }
-                put_items<V, WHOLE>(items, t.r, nv, cv, k, s1, s2);
-                if (t.rows > 1 || nv <= TDC_NORM_THREADS) {
+                if (nv <= TDC_NORM_THREADS) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         t1[v] += s1[v];
@@ -300,19 +301,17 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDi
                         row[v] = make_float2(o.x + s1[v], o.y + s2[v]);
                     }
                 }
-                if (t.rows > 1) break;
             }
+            rows = put_items<V, WHOLE, TDC_NORM_THREADS>(items, t, cv, nv, live, used, k, s1, s2);
+            if (t.rows > 1) break;
+        }
         __syncthreads();
         float2 *to = partial + ((size_t)b * d.chunks + chunk) * d.G;
-        tdc_norm_group_sums(items, used, d.G, WHOLE ? d.Cg / V : d.Cg, TDC_NORM_THREADS, [&](int g, float s1, float s2) { to[g] = make_float2(s1, s2); });
+        tdc_norm_group_sums(items, rows, d.G, WHOLE ? d.Cg / V : d.Cg, TDC_NORM_THREADS, [&](int g, float s1, float s2) { to[g] = make_float2(s1, s2); });
         __syncthreads();
     }
     if (!sums || nv > TDC_NORM_THREADS) return;
-    if (t.r < used && t.cv < nv) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) items[(t.r * nv + t.cv) * V + v] = make_float2(t1[v], t2[v]);
-    }
-    add_rows(items, used, d.C, sums + (size_t)(blockIdx.y * gridDim.x + chunk) * d.C, TDC_NORM_THREADS);
+    add_rows<V, TDC_NORM_THREADS>(items, t1, t2, t, nv, t.r < used && t.cv < nv, used, sums + (size_t)(blockIdx.y * gridDim.x + chunk) * d.C);
 }
 
 // ---- gradients of chunks: grid (chunks, batch), and behind them the workgroups that add up the channels' sums
@@ -353,12 +352,10 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormD
         k.weights(q, cv * V);
         k.statistics(d, q, b, cv * V);
         float m1[V], m2[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float2 m = means[(cv * V + v) / d.Cg];
-            m1[v] = m.x;
-            m2[v] = m.y;
-        }
+        tdc_norm_channels<V>(cv * V, d.Cg, [&](int v, int g) {
+            m1[v] = means[g].x;
+            m2[v] = means[g].y;
+        });
         for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
             TdcVec<T, V> xv[U], dv[U], rv[U];
 #pragma unroll
@@ -407,10 +404,10 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
     const TdcNormSlice sl = tdc_norm_slice(d, dt, vec, true, 1);
     if (sl.held) {
         const int rows = std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / sl.slices));
-        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), true), THREADS, HELD, {
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, 512, tdc_norm_held(V, sizeof(T), true), THREADS, HELD, {
             const unsigned wgs = (unsigned)rows * sl.slices;
-            if (whole) tdc_norm_grad_resident<T, V, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sums);
-            else tdc_norm_grad_resident<T, V, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sums);
+            if (whole) tdc_norm_grad_resident<T, V, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sl.held, sums);
+            else tdc_norm_grad_resident<T, V, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sl.held, sums);
         })));
         if (sums) tdc_norm_grad_weights<256><<<weight_blocks, 256, 0, s>>>(d.C, sums, rows, dgamma, dbeta);
         return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;

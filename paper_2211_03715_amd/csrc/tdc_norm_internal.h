@@ -69,7 +69,9 @@ __host__ __device__ inline int tdc_team(int groups, int terms, int threads)
 // A thread takes its V channels of several pixels at a time into registers, their mean and the squares about it, and merges that
 // into what it has (n_a, mean_a, S_a with n_b, mean_b, S_b: mean = mean_a + d n_b / n, S = S_a + S_b + d^2 n_a n_b / n,
 // d = mean_b - mean_a).  No sum of squares is ever taken about anything but a mean next to the values, so fp32 does.
-template <int V> struct TdcNormSums {
+// From there on it has I items: its piece as a whole where the channels are of one group (WHOLE), or every channel by itself.
+template <int V, bool WHOLE> struct TdcNormSums {
+    static constexpr int I = WHOLE ? 1 : V;
     float n, mean[V], m2[V];
     __device__ __forceinline__ TdcNormSums()
     {
@@ -77,19 +79,19 @@ template <int V> struct TdcNormSums {
 #pragma unroll
         for (int v = 0; v < V; ++v) mean[v] = m2[v] = 0.f;
     }
-    // the first k of U pixels
-    template <typename T, int U> __device__ __forceinline__ void add(const TdcVec<T, V> (&in)[U], int k)
+    // pixel i of `in` counts where i < k; FULL: all of them do
+    template <bool FULL, typename T, int U> __device__ __forceinline__ void add_some(const TdcVec<T, V> (&in)[U], int k)
     {
-        const float inv_k = 1.f / k, tot = n + k, w = k / tot;
+        const float inv_k = FULL ? 1.f / U : 1.f / k, tot = n + k, w = k * __builtin_amdgcn_rcpf(tot);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float s = 0.f, q = 0.f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) s += u < k ? (float)in[u].v[v] : 0.f;
+            for (int u = 0; u < U; ++u) s += FULL || u < k ? (float)in[u].v[v] : 0.f;
             s *= inv_k;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float off = u < k ? (float)in[u].v[v] - s : 0.f;
+                const float off = FULL || u < k ? (float)in[u].v[v] - s : 0.f;
                 q += off * off;
             }
             const float off = s - mean[v];
@@ -98,72 +100,186 @@ template <int V> struct TdcNormSums {
         }
         n = tot;
     }
-    // as an item to combine: the piece as a whole (WHOLE: its channels are of one group), or every channel by itself
-    template <bool WHOLE> __device__ __forceinline__ void put(float2 *items, int row, int nv, int cv) const
+    template <typename T, int U> __device__ __forceinline__ void add(const TdcVec<T, V> (&in)[U], int k)
     {
-        if constexpr (WHOLE) {
-            float m = 0.f, q = 0.f;
+        if (k == U) add_some<true>(in, U);
+        else add_some<false>(in, k);
+    }
+    __device__ __forceinline__ void merge(float n_b, const float (&mean_b)[I], const float (&m2_b)[I])
+    {
+        const float tot = n + n_b, w = tot > 0.f ? n_b * __builtin_amdgcn_rcpf(tot) : 0.f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) m += mean[v];
-            m *= 1.f / V;
-#pragma unroll
-            for (int v = 0; v < V; ++v) q += m2[v] + (mean[v] - m) * (mean[v] - m) * n;
-            items[row * nv + cv] = make_float2(m, q);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) items[(row * nv + cv) * V + v] = make_float2(mean[v], m2[v]);
+        for (int i = 0; i < I; ++i) {
+            const float off = mean_b[i] - mean[i];
+            mean[i] += off * w;
+            m2[i] += m2_b[i] + off * off * (n * w);
         }
+        n = tot;
     }
 };
 
-// The items of a workgroup's `used` rows (row r over full + (r < rem) pixels) combined group by group, a team of lanes to a
-// group: f(g, values, mean, squares about it) in one lane of it.  per_group items of `width` channels to a row and group.
-template <typename F> __device__ __forceinline__ void tdc_norm_groups(const float2 *items, int used, int full, int rem, int groups, int per_group, int width, int threads, F f)
+// Items in LDS: `rows` rows of nv pieces, with the values that an item of the row stands for.  Where nv is a power of two below
+// 64, a row is what a wavefront's lanes of the same piece have together, else what a pixel row of threads has.
+struct TdcNormItems {
+    float2 *item;
+    float *count;
+};
+
+__device__ __forceinline__ bool tdc_norm_by_wave(int nv) { return nv < 64 && (nv & (nv - 1)) == 0; }
+
+// Every thread of the workgroup calls this, `live` ones with the sums of piece cv, the others with none (n = 0); or those with
+// one, where nv >= 64.  Returns the number of rows.  The caller synchronises.
+template <int V, bool WHOLE, int THREADS>
+__device__ __forceinline__ int tdc_norm_put(const TdcNormItems &to, TdcNormSums<V, WHOLE> &s, const TdcNormLanes &t, int cv, int nv, bool live, int used)
 {
-    const int L = tdc_team(groups, used * per_group, threads), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = threads / L;
-    const int pitch = groups * per_group, terms = used * per_group;
-    for (int g0 = 0; g0 < groups; g0 += teams) {       // the same trip count for every lane: lane sums need all of a team
-        const int g = min(g0 + team, groups - 1);
+    constexpr int I = TdcNormSums<V, WHOLE>::I;
+    if (WHOLE) {
+        float m = 0.f, q = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) m += s.mean[v];
+        m *= 1.f / V;
+#pragma unroll
+        for (int v = 0; v < V; ++v) q += s.m2[v] + (s.mean[v] - m) * (s.mean[v] - m) * s.n;
+        s.mean[0] = m;
+        s.m2[0] = q;
+        s.n *= V;
+    }
+    int row = t.r, rows = used;
+    bool writes = live;
+    if (tdc_norm_by_wave(nv)) {
+        tdc_merge_lanes(nv, [&](auto first, auto second) {
+            float mean[I], m2[I];
+            const float n = second(s.n);
+            s.n = first(s.n);
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                mean[i] = second(s.mean[i]);
+                m2[i] = second(s.m2[i]);
+                s.mean[i] = first(s.mean[i]);
+                s.m2[i] = first(s.m2[i]);
+            }
+            s.merge(n, mean, m2);
+        });
+        row = threadIdx.x / 64;
+        rows = THREADS / 64;
+        writes = (threadIdx.x & 63) < nv;
+    }
+    if (writes) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) to.item[(row * nv + cv) * I + i] = make_float2(s.mean[i], s.m2[i]);
+        if (cv == 0) to.count[row] = s.n;
+    }
+    return rows;
+}
+
+// How a team of L lanes lies over `rows` x `per_group` items: powers of two, so that no index needs a division.
+struct TdcNormTeam {
+    int L, lane, team, teams, k0, kstep, r0, rstep;
+    __device__ __forceinline__ TdcNormTeam(int groups, int rows, int per_group, int threads)
+    {
+        L = tdc_team(groups, rows * per_group, threads);
+        lane = threadIdx.x & (L - 1);
+        team = threadIdx.x / L;
+        teams = threads / L;
+        kstep = 1;
+        while (kstep < per_group && kstep < L) kstep *= 2;
+        k0 = lane & (kstep - 1);
+        rstep = L / kstep;
+        r0 = lane / kstep;
+    }
+};
+
+// The items combined group by group, a team of lanes to a group: f(g, values, mean, squares about it) in one lane of it.
+template <int THREADS, typename F> __device__ __forceinline__ void tdc_norm_groups(const TdcNormItems &from, int rows, int groups, int per_group, F f)
+{
+    const TdcNormTeam t(groups, rows, per_group, THREADS);
+    const int pitch = groups * per_group;
+    for (int g0 = 0; g0 < groups; g0 += t.teams) {     // the same trip count for every lane: lane sums need all of a team
+        const int g = min(g0 + t.team, groups - 1);
         float n = 0.f, s = 0.f;
-        for (int i = lane; i < terms; i += L) {
-            const int row = i / per_group;
-            const float k = (float)((full + (row < rem)) * width);
-            n += k;
-            s += k * items[row * pitch + g * per_group + i - row * per_group].x;
+        for (int r = t.r0; r < rows; r += t.rstep) {
+            const float c = from.count[r];
+            if (c > 0.f)
+                for (int k = t.k0; k < per_group; k += t.kstep) {
+                    n += c;
+                    s += c * from.item[r * pitch + g * per_group + k].x;
+                }
         }
-        n = tdc_lane_sum(n, L);
-        const float mean = tdc_lane_sum(s, L) / n;
+        n = tdc_lane_sum(n, t.L);
+        const float mean = tdc_lane_sum(s, t.L) / n;
         float m2 = 0.f;
-        for (int i = lane; i < terms; i += L) {
-            const int row = i / per_group;
-            const float2 o = items[row * pitch + g * per_group + i - row * per_group];
-            m2 += o.y + (o.x - mean) * (o.x - mean) * (float)((full + (row < rem)) * width);
+        for (int r = t.r0; r < rows; r += t.rstep) {
+            const float c = from.count[r];
+            if (c > 0.f)
+                for (int k = t.k0; k < per_group; k += t.kstep) {
+                    const float2 o = from.item[r * pitch + g * per_group + k];
+                    m2 += o.y + (o.x - mean) * (o.x - mean) * c;
+                }
         }
-        m2 = tdc_lane_sum(m2, L);
-        if (lane == 0 && g0 + team < groups) f(g, n, mean, m2);
+        m2 = tdc_lane_sum(m2, t.L);
+        if (t.lane == 0 && g0 + t.team < groups) f(g, n, mean, m2);
+    }
+}
+
+// Group of each of V neighbouring channels from c0 on, f(v, group): one division, whatever V is.
+template <int V, typename F> __device__ __forceinline__ void tdc_norm_channels(int c0, int Cg, F f)
+{
+    int g = c0 / Cg, rest = c0 - g * Cg;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        f(v, g);
+        if (++rest == Cg) {
+            rest = 0;
+            ++g;
+        }
     }
 }
 
 __device__ __forceinline__ float tdc_rstd(float var, float eps) { return 1.f / sqrtf(var + eps); }
 
-// The same rows' items as plain sums.
-template <typename F> __device__ __forceinline__ void tdc_norm_group_sums(const float2 *items, int used, int groups, int per_group, int threads, F f)
+// The same for items that are plain sums: [rows][groups * per_group].
+template <typename F> __device__ __forceinline__ void tdc_norm_group_sums(const float2 *items, int rows, int groups, int per_group, int threads, F f)
 {
-    const int L = tdc_team(groups, used * per_group, threads), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = threads / L;
-    const int pitch = groups * per_group, terms = used * per_group;
-    for (int g0 = 0; g0 < groups; g0 += teams) {
-        const int g = min(g0 + team, groups - 1);
+    const TdcNormTeam t(groups, rows, per_group, threads);
+    const int pitch = groups * per_group;
+    for (int g0 = 0; g0 < groups; g0 += t.teams) {
+        const int g = min(g0 + t.team, groups - 1);
         float s1 = 0.f, s2 = 0.f;
-        for (int i = lane; i < terms; i += L) {
-            const int row = i / per_group;
-            const float2 o = items[row * pitch + g * per_group + i - row * per_group];
-            s1 += o.x;
-            s2 += o.y;
-        }
-        s1 = tdc_lane_sum(s1, L);
-        s2 = tdc_lane_sum(s2, L);
-        if (lane == 0 && g0 + team < groups) f(g, s1, s2);
+        for (int r = t.r0; r < rows; r += t.rstep)
+            for (int k = t.k0; k < per_group; k += t.kstep) {
+                const float2 o = items[r * pitch + g * per_group + k];
+                s1 += o.x;
+                s2 += o.y;
+            }
+        s1 = tdc_lane_sum(s1, t.L);
+        s2 = tdc_lane_sum(s2, t.L);
+        if (t.lane == 0 && g0 + t.team < groups) f(g, s1, s2);
     }
+}
+
+// Plain sums of I items to a thread into LDS, lanes of a wavefront with the same piece together where tdc_norm_by_wave says so.
+// Returns the number of rows.  The caller synchronises.
+template <int I, int THREADS> __device__ __forceinline__ int tdc_norm_put_sums(float2 *items, float (&s1)[I], float (&s2)[I], const TdcNormLanes &t, int cv, int nv, bool live, int used)
+{
+    int row = t.r, rows = used;
+    bool writes = live;
+    if (tdc_norm_by_wave(nv)) {
+        tdc_merge_lanes(nv, [&](auto first, auto second) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                s1[i] = first(s1[i]) + second(s1[i]);
+                s2[i] = first(s2[i]) + second(s2[i]);
+            }
+        });
+        row = threadIdx.x / 64;
+        rows = THREADS / 64;
+        writes = (threadIdx.x & 63) < nv;
+    }
+    if (writes) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) items[(row * nv + cv) * I + i] = make_float2(s1[i], s2[i]);
+    }
+    return rows;
 }
 
 // The chunks' sums of image b as {mean, rstd} of every group into `stats` [G] in LDS.  Every thread of the workgroup calls it.
@@ -207,17 +323,16 @@ inline int tdc_norm_vec(int dtype, int C, std::initializer_list<int64_t> pitches
 
 // ---- the resident form
 
-// Pieces of x that a thread holds at most: 64 values of fp32, fewer where the conversions need the registers, and fewer still
-// backward, where dy is held too.  Twice as many spill.
-__host__ __device__ constexpr int tdc_norm_held(int V, int size, bool backward) { return backward ? 4 : (V >= 4 && size == 2 ? 8 : 16); }
+// Pieces of x that a thread holds at most.  Forward, 1024 threads have 128 registers each: 64 values of fp32, 32 of 16 bits that
+// have to be converted.  Backward, where d is held too, in fp32, 512 threads have 256.
+__host__ __device__ constexpr int tdc_norm_held(int V, int size, bool backward) { return backward ? 8 : (V >= 4 && size == 2 ? 8 : 16); }
 
 // A workgroup takes `width` channels, whole groups and whole pieces, of an image; `slices` of them to an image.
 struct TdcNormSlice {
     int width, slices, threads, held;    // held: pieces to a thread; 0: the image does not fit
 };
 
-// Slices are lines of 128 bytes where a workgroup's registers hold that much (two workgroups of 512 threads to a compute unit,
-// or one of 1024), and else less, down to one group.  A line that two or four workgroups share comes from memory once all the
+// Slices are lines of 128 bytes where a workgroup's registers hold that much, and else less, down to one group.  A line that two or four workgroups share comes from memory once all the
 // same: they run on the same XCD (tdc_norm_place).
 inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool backward, int multiple)
 {
@@ -238,9 +353,9 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool 
         const int line = width * tdc_dtype_bytes(dtype);
         if (best.held && line > 128) break;
         for (int threads : {256, 512, 1024}) {
-            const int held = fits(width, threads);
-            if (held > most) continue;
-            if (held > 4 && threads < 1024) continue;   // rather more threads than more to each
+            const int held = fits(width, threads), top = backward ? 512 : 1024;
+            if (held > most || threads > top) continue;
+            if (held > 4 && threads < top) continue;    // rather more threads than more to each
             best = TdcNormSlice{width, d.C / width, threads, held};
             break;
         }
@@ -260,14 +375,14 @@ __device__ __forceinline__ void tdc_norm_place(int id, int total, int slices, in
     slice = t - b * slices;
 }
 
-// The statements with the constants THREADS and HELD that a slice asks for; MOST is what tdc_norm_held says.
-#define TDC_FOR_SLICE(s, MOST, THREADS, HELD, ...)                                                                                  \
+// The statements with the constants THREADS and HELD that a slice asks for; TOP is the most threads, MOST what tdc_norm_held says.
+#define TDC_FOR_SLICE(s, TOP, MOST, THREADS, HELD, ...)                                                                             \
     do {                                                                                                                            \
         if ((s).threads == 256) { constexpr int THREADS = 256, HELD = 4; __VA_ARGS__; }                                             \
-        else if ((s).threads == 512) { constexpr int THREADS = 512, HELD = 4; __VA_ARGS__; }                                        \
-        else if ((s).held <= 4) { constexpr int THREADS = 1024, HELD = 4; __VA_ARGS__; }                                            \
-        else if ((s).held <= 8) { if constexpr ((MOST) >= 8) { constexpr int THREADS = 1024, HELD = 8; __VA_ARGS__; } }             \
-        else if constexpr ((MOST) >= 16) { constexpr int THREADS = 1024, HELD = 16; __VA_ARGS__; }                                  \
+        else if ((s).threads == 512 && (s).held <= 4) { constexpr int THREADS = 512, HELD = 4; __VA_ARGS__; }                       \
+        else if ((s).held <= 4) { if constexpr ((TOP) == 1024) { constexpr int THREADS = 1024, HELD = 4; __VA_ARGS__; } }           \
+        else if ((s).held <= 8) { constexpr int THREADS = TOP, HELD = 8; __VA_ARGS__; }                                             \
+        else if constexpr ((MOST) >= 16) { constexpr int THREADS = TOP, HELD = 16; __VA_ARGS__; }                                   \
     } while (0)
 
 #endif  // TDC_NORM_INTERNAL_H

@@ -87,11 +87,71 @@ template <int ACT> __device__ __forceinline__ float tdc_activate_grad(float v)
     return 1.f;
 }
 
-// Sum over the neighbouring `lanes` lanes (a power of two up to 64), the same in each of them.
+// ---- lanes of a wavefront, without a trip through LDS
+
+// The value of another lane of a row of 16; the constants are the ISA's (quad_perm, row_half_mirror, row_mirror, row_ror:n).
+template <int CTRL> __device__ __forceinline__ float tdc_dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+constexpr int TDC_DPP_XOR1 = 0xb1, TDC_DPP_XOR2 = 0x4e, TDC_DPP_HALF_MIRROR = 0x141, TDC_DPP_MIRROR = 0x140, TDC_DPP_ROR = 0x120;
+
+// What the two rows of 16 of every 32 lanes hold, and the two halves of the 64: lane by lane, the same pair in both.
+__device__ __forceinline__ float2 tdc_rows16(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];
+    return make_float2(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float2 tdc_rows32(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];
+    return make_float2(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+// Sum over the neighbouring `lanes` lanes (a power of two up to 64), the same in each of them.  The mirrors do for exchanges of 4
+// and 8 lanes: what they swap is the same in all four or eight.
 __device__ __forceinline__ float tdc_lane_sum(float v, int lanes)
 {
-    for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o, 64);
+    if (lanes > 1) v += tdc_dpp<TDC_DPP_XOR1>(v);
+    if (lanes > 2) v += tdc_dpp<TDC_DPP_XOR2>(v);
+    if (lanes > 4) v += tdc_dpp<TDC_DPP_HALF_MIRROR>(v);
+    if (lanes > 8) v += tdc_dpp<TDC_DPP_MIRROR>(v);
+    if (lanes > 16) {
+        const float2 r = tdc_rows16(v);
+        v = r.x + r.y;
+    }
+    if (lanes > 32) {
+        const float2 r = tdc_rows32(v);
+        v = r.x + r.y;
+    }
     return v;
+}
+
+// The largest of unsigned bits over 4 or 8 neighbouring lanes.
+template <int LANES> __device__ __forceinline__ unsigned tdc_lane_max(unsigned u)
+{
+    u = max(u, __builtin_bit_cast(unsigned, tdc_dpp<TDC_DPP_XOR1>(__builtin_bit_cast(float, u))));
+    u = max(u, __builtin_bit_cast(unsigned, tdc_dpp<TDC_DPP_XOR2>(__builtin_bit_cast(float, u))));
+    if (LANES > 4) u = max(u, __builtin_bit_cast(unsigned, tdc_dpp<TDC_DPP_HALF_MIRROR>(__builtin_bit_cast(float, u))));
+    return u;
+}
+
+// f(first, second) over the lanes that are `from`, 2 `from`, ... apart, `from` a power of two below 64: first(v) is a lane's own
+// value of v, second(v) another's, and what f leaves is merged further.  Below 16 apart lanes of a row go around, so lanes merge
+// in orders of their own; the lanes below `from` are those to read.
+template <typename F> __device__ __forceinline__ void tdc_merge_lanes(int from, F f)
+{
+    const auto own = [](float v) { return v; };
+    if (from <= 1) f(own, [](float v) { return tdc_dpp<TDC_DPP_ROR + 1>(v); });
+    if (from <= 2) f(own, [](float v) { return tdc_dpp<TDC_DPP_ROR + 2>(v); });
+    if (from <= 4) f(own, [](float v) { return tdc_dpp<TDC_DPP_ROR + 4>(v); });
+    if (from <= 8) f(own, [](float v) { return tdc_dpp<TDC_DPP_ROR + 8>(v); });
+    if (from <= 16) f([](float v) { return tdc_rows16(v).x; }, [](float v) { return tdc_rows16(v).y; });
+    if (from <= 32) f([](float v) { return tdc_rows32(v).x; }, [](float v) { return tdc_rows32(v).y; });
 }
 
 // The statements for a dtype with T its type, for an activation with the constant ACT, for V neighbours with the constant V.
