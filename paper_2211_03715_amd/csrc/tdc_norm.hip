@@ -66,7 +66,7 @@ template <int V> __device__ __forceinline__ void store_mx4(const NormOut &out, c
 
 // ---- resident: a slice of an image's channels in the registers of a workgroup
 template <typename T, int V, bool WHOLE, bool MX4, int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS) void tdc_norm_resident(TdcNormDims d, NormIn in, NormOut out, int width, int slices, int held_here)
+__global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, NormIn in, NormOut out, int width, int slices, int held_here)
 {
     __shared__ float2 item[THREADS * (WHOLE ? 1 : V)], stats[THREADS];
     __shared__ float count[THREADS];
@@ -148,42 +148,80 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_stats(TdcNormDims d
     tdc_norm_groups<TDC_NORM_THREADS>(items, rows, d.G, WHOLE ? d.Cg / V : d.Cg, [&](int g, float n, float mean, float m2) { out[g] = make_float4(n, mean, m2, 0.f); });
 }
 
+// ---- an image's chunks in one: a wavefront to a group, grid (groups, batch)
+__global__ __launch_bounds__(64) void tdc_norm_combine(TdcNormDims d, const float4 *__restrict__ partial, float4 *__restrict__ whole)
+{
+    const size_t b = blockIdx.y, g = blockIdx.x;
+    const float4 *p = partial + b * d.chunks * d.G + g;
+    float n = 0.f, s = 0.f, m2 = 0.f;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < d.chunks; i += 64) {
+        const float4 o = p[(size_t)i * d.G];
+        n += o.x;
+        s += o.x * o.y;
+    }
+    n = tdc_lane_sum(n, 64);
+    const float mean = tdc_lane_sum(s, 64) / n;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < d.chunks; i += 64) {
+        const float4 o = p[(size_t)i * d.G];
+        m2 += o.z + o.x * (o.y - mean) * (o.y - mean);
+    }
+    m2 = tdc_lane_sum(m2, 64);
+    if (threadIdx.x == 0) whole[b * d.G + g] = make_float4(n, mean, m2, 0.f);
+}
+
+// {mean, rstd} of every group of image b into `stats` [G] in LDS; the workgroup of the first chunk writes them out.
+__device__ __forceinline__ void statistics(const TdcNormDims &d, const NormOut &out, const float4 *partial, int parts, int b, int chunk, float2 *stats)
+{
+    tdc_combine(d, partial, parts, b, TDC_NORM_THREADS, [&](int g, float n, float mean, float m2) {
+        const float rstd = tdc_rstd(m2 / n, d.eps);
+        stats[g] = make_float2(mean, rstd);
+        if (chunk) return;
+        if (out.mean) out.mean[(size_t)b * d.G + g] = mean;
+        if (out.rstd) out.rstd[(size_t)b * d.G + g] = rstd;
+    });
+    __syncthreads();
+}
+
 // ---- y = act((x - mean) * (rstd gamma) + beta + residual): grid (chunks, batch)
 template <typename T, int V, bool MX4>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial)
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial, int parts)
 {
-    constexpr int U = TDC_NORM_UNROLL;
+    constexpr int U = 2;
     extern __shared__ float2 stats[];                      // [G]
     const int nv = d.C / V, b = blockIdx.y, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
-    tdc_combine_chunks(d, partial, b, stats, TDC_NORM_THREADS);
-    if (chunk == 0)
-        for (int g = threadIdx.x; g < d.G; g += TDC_NORM_THREADS) {
-            if (out.mean) out.mean[(size_t)b * d.G + g] = stats[g].x;
-            if (out.rstd) out.rstd[(size_t)b * d.G + g] = stats[g].y;
-        }
     const TdcNormLanes t(nv, TDC_NORM_THREADS);
     const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
     const T *x = static_cast<const T *>(in.x) + first * in.xp, *res = in.residual ? static_cast<const T *>(in.residual) + first * in.rp : nullptr;
+    TdcVec<T, V> v[U], rv[U];
+    auto fetch = [&](int cv, int p0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(x + (size_t)min(p0 + u * t.rows, len - 1) * in.xp + cv * V);
+        if (res) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) rv[u] = tdc_load<T, V>(res + (size_t)min(p0 + u * t.rows, len - 1) * in.rp + cv * V);
+        }
+    };
+    // the first pixels are on their way while the statistics are put together
+    if (t.r < t.rows && t.cv < nv) fetch(t.cv, t.r);
+    statistics(d, out, partial, parts, b, chunk, stats);
     // MX4: the lanes of a block go through the loops together (nv is a multiple of 32 / V)
     if (t.r >= t.rows) return;
     for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
         Affine<V> a;
         a.set(d, in, stats, 0, cv * V);
+        if (cv != t.cv) fetch(cv, t.r);
         for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
-            TdcVec<T, V> v[U], rv[U];
+            float o[U][V];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(x + (size_t)min(p0 + u * t.rows, len - 1) * in.xp + cv * V);
-            if (res) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) rv[u] = tdc_load<T, V>(res + (size_t)min(p0 + u * t.rows, len - 1) * in.rp + cv * V);
-            }
+            for (int u = 0; u < U; ++u) apply(a, v[u], rv[u], in, o[u]);
+            if (p0 + t.rows * U < len) fetch(cv, p0 + t.rows * U);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int p = p0 + u * t.rows;
-                float o[V];
-                apply(a, v[u], rv[u], in, o);
-                if constexpr (MX4) store_mx4<V>(out, o, first + p, (d.C + 31) / 32, cv * V, p < len);
-                else if (p < len) tdc_store<T, V>(static_cast<T *>(out.y) + (first + p) * out.pitch + cv * V, o);
+                if constexpr (MX4) store_mx4<V>(out, o[u], first + p, (d.C + 31) / 32, cv * V, p < len);
+                else if (p < len) tdc_store<T, V>(static_cast<T *>(out.y) + (first + p) * out.pitch + cv * V, o[u]);
             }
         }
         if (t.rows > 1) break;
@@ -192,16 +230,11 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d
 
 // ---- the same, written in 4 bits, where C is no multiple of 32: a thread takes a block of 32 channels of a pixel
 template <typename T, int V>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_blocks(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial)
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_blocks(TdcNormDims d, NormIn in, NormOut out, const float4 *__restrict__ partial, int parts)
 {
     extern __shared__ float2 stats[];                      // [G]
     const int b = blockIdx.y, chunk = blockIdx.x;
-    tdc_combine_chunks(d, partial, b, stats, TDC_NORM_THREADS);
-    if (chunk == 0)
-        for (int g = threadIdx.x; g < d.G; g += TDC_NORM_THREADS) {
-            if (out.mean) out.mean[(size_t)b * d.G + g] = stats[g].x;
-            if (out.rstd) out.rstd[(size_t)b * d.G + g] = stats[g].y;
-        }
+    statistics(d, out, partial, parts, b, chunk, stats);
     const int nb = (d.C + 31) / 32;
     const T *x = static_cast<const T *>(in.x), *res = static_cast<const T *>(in.residual);
     const size_t total = (size_t)tdc_chunk_len(d, chunk) * nb, first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
@@ -239,13 +272,13 @@ int validate(const tdc_norm_shape &s)
     return TDC_OK;
 }
 
-// Pixels to a chunk: two workgroups to a compute unit over the batch, but no less than one round of a workgroup's threads.
+// Pixels to a chunk: four workgroups to a compute unit over the batch, but no less than two pieces to a thread.
 void choose_chunks(TdcNormDims &d, int dtype)
 {
     const int pieces = (d.C * tdc_dtype_bytes(dtype) + 15) / 16;
     const int rows = pieces < TDC_NORM_THREADS ? TDC_NORM_THREADS / pieces : 1;
-    const int most = d.B >= 512 ? 1 : 512 / d.B;
-    const int64_t chunks = std::min<int64_t>(most, ((int64_t)d.P + TDC_NORM_UNROLL * rows - 1) / (TDC_NORM_UNROLL * rows));
+    const int most = d.B >= 1024 ? 1 : 1024 / d.B;
+    const int64_t chunks = std::min<int64_t>(most, ((int64_t)d.P + 2 * rows - 1) / (2 * rows));
     d.chunk_px = (int)((d.P + chunks - 1) / chunks);
     d.chunks = (d.P + d.chunk_px - 1) / d.chunk_px;
 }
@@ -273,14 +306,15 @@ int tdc_norm_plan_create(tdc_norm_plan **out, const tdc_norm_shape *shape, int d
     p->dims = TdcNormDims{shape->batch, shape->H * shape->W, shape->C, shape->groups, shape->C / shape->groups, 0, 0, shape->eps};
     choose_chunks(p->dims, shape->dtype);
     const size_t groups = (size_t)p->dims.B * p->dims.G, partials = groups * p->dims.chunks;
-    const size_t sums = std::min<size_t>((size_t)p->dims.B * p->dims.chunks, TDC_NORM_SUM_ROWS) * p->dims.C;
-    p->ws_bytes = partials * sizeof(float4) + sums * sizeof(float2);
+    const size_t sums = tdc_norm_sum_rows(p->dims) * p->dims.C;
+    p->ws_bytes = (partials + groups) * sizeof(float4) + sums * sizeof(float2);
     if (hipMalloc((void **)&p->partial, p->ws_bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete p;
         return TDC_ERR_ALLOC;
     }
-    p->sums = reinterpret_cast<float2 *>(p->partial + partials);
+    p->whole = p->partial + partials;
+    p->sums = reinterpret_cast<float2 *>(p->whole + groups);
     *out = p;
     return TDC_OK;
 }
@@ -300,7 +334,7 @@ int tdc_norm_plan_kernel_count(const tdc_norm_plan *p)
 {
     if (!p) return 0;
     const int V = tdc_norm_vec(p->shape.dtype, p->dims.C, {}, {});
-    return tdc_norm_slice(p->dims, p->shape.dtype, V, false, 1).held ? 1 : 2;
+    return tdc_norm_slice(p->dims, p->shape.dtype, V, false, 1).held ? 1 : p->dims.chunks > TDC_NORM_PARTS ? 3 : 2;
 }
 
 }  // extern "C"
@@ -329,7 +363,7 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);
     if (sl.held) {
-        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC(V0, T, V, TDC_FOR_SLICE(sl, 1024, tdc_norm_held(V, sizeof(T), false), THREADS, HELD, {
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC(V0, T, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), false), true, THREADS, HELD, {
             const unsigned wgs = (unsigned)d.B * sl.slices;
             if (lanes) {
                 if constexpr (V * sizeof(T) == 16) {
@@ -350,11 +384,15 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
             if (whole_x) tdc_norm_stats<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
             else tdc_norm_stats<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
         });
+        const bool between = d.chunks > TDC_NORM_PARTS;
+        if (between) tdc_norm_combine<<<dim3(d.G, d.B), 64, 0, s>>>(d, p->partial, p->whole);
+        const float4 *sums = between ? p->whole : p->partial;
+        const int parts = between ? 1 : d.chunks;
         TDC_FOR_VEC(V0, T, V, {
             const size_t lds = d.G * sizeof(float2);
-            if (y) tdc_norm_apply<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
-            else if (!lanes) tdc_norm_apply_blocks<T, V><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
-            else if constexpr (V * sizeof(T) == 16) tdc_norm_apply<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, p->partial);
+            if (y) tdc_norm_apply<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
+            else if (!lanes) tdc_norm_apply_blocks<T, V><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
+            else if constexpr (V * sizeof(T) == 16) tdc_norm_apply<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
         });
     });
     return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;

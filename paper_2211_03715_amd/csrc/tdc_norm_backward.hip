@@ -158,6 +158,29 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void tdc_norm_grad_
     add_weights<THREADS>(C, sums, rows, blockIdx.x * 32, dgamma, dbeta);
 }
 
+// An image's chunks in one, a wavefront to a group, and behind them the workgroups that add up the channels' sums.
+__global__ __launch_bounds__(256) void tdc_norm_grad_combine(TdcNormDims d, const float2 *__restrict__ partial, float2 *__restrict__ whole, int wgs, const float2 *__restrict__ sums,
+                                                             int rows, float *__restrict__ dgamma, float *__restrict__ dbeta)
+{
+    if ((int)blockIdx.x >= wgs) {
+        add_weights<256>(d.C, sums, rows, (blockIdx.x - wgs) * 32, dgamma, dbeta);
+        return;
+    }
+    const size_t at = (size_t)blockIdx.x * 4 + threadIdx.x / 64, b = at / d.G, g = at - b * d.G;
+    if (b >= (size_t)d.B) return;
+    const float2 *p = partial + b * d.chunks * d.G + g;
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll 8
+    for (int i = threadIdx.x & 63; i < d.chunks; i += 64) {
+        const float2 o = p[(size_t)i * d.G];
+        s1 += o.x;
+        s2 += o.y;
+    }
+    s1 = tdc_lane_sum(s1, 64);
+    s2 = tdc_lane_sum(s2, 64);
+    if ((threadIdx.x & 63) == 0) whole[at] = make_float2(s1, s2);
+}
+
 // ---- resident: workgroup (row, slice) takes images row, row + rows_of_images, ...
 // After the sums a thread keeps x and d, in fp32: the residual is read once, the activation's slope computed once.
 template <typename T, int V, bool WHOLE, int THREADS, int HELD>
@@ -316,7 +339,7 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDi
 
 // ---- gradients of chunks: grid (chunks, batch), and behind them the workgroups that add up the channels' sums
 template <typename T, int V>
-__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormDims d, GradIn q, GradOut out, const float2 *__restrict__ partial, const float2 *__restrict__ sums, int rows,
+__global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormDims d, GradIn q, GradOut out, const float2 *__restrict__ partial, int parts, const float2 *__restrict__ sums, int rows,
                                                                          float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
     constexpr int U = TDC_NORM_UNROLL / 2;
@@ -327,21 +350,8 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormD
         return;
     }
     const int nv = d.C / V, len = tdc_chunk_len(d, chunk);
-    const int L = tdc_team(d.G, d.chunks, TDC_NORM_THREADS), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = TDC_NORM_THREADS / L;
     const float inv = 1.f / ((float)d.P * d.Cg);
-    for (int g0 = 0; g0 < d.G; g0 += teams) {
-        const int g = min(g0 + team, d.G - 1);
-        const float2 *p = partial + (size_t)b * d.chunks * d.G + g;
-        float s1 = 0.f, s2 = 0.f;
-        for (int i = lane; i < d.chunks; i += L) {
-            const float2 o = p[(size_t)i * d.G];
-            s1 += o.x;
-            s2 += o.y;
-        }
-        s1 = tdc_lane_sum(s1, L);
-        s2 = tdc_lane_sum(s2, L);
-        if (lane == 0 && g0 + team < d.G) means[g] = make_float2(s1 * inv, s2 * inv);
-    }
+    tdc_combine_sums(d, partial, parts, b, TDC_NORM_THREADS, [&](int g, float s1, float s2) { means[g] = make_float2(s1 * inv, s2 * inv); });
     __syncthreads();
     const TdcNormLanes t(nv, TDC_NORM_THREADS);
     if (t.r >= t.rows) return;
@@ -403,8 +413,8 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
     const bool whole = d.Cg % vec == 0;
     const TdcNormSlice sl = tdc_norm_slice(d, dt, vec, true, 1);
     if (sl.held) {
-        const int rows = std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / sl.slices));
-        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, 512, tdc_norm_held(V, sizeof(T), true), THREADS, HELD, {
+        const int rows = tdc_norm_resident_rows(d, sl.slices);
+        TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), true), false, THREADS, HELD, {
             const unsigned wgs = (unsigned)rows * sl.slices;
             if (whole) tdc_norm_grad_resident<T, V, true, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sl.held, sums);
             else tdc_norm_grad_resident<T, V, false, THREADS, HELD><<<wgs, THREADS, 0, s>>>(d, q, out, sl.width, sl.slices, sl.held, sums);
@@ -412,7 +422,7 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
         if (sums) tdc_norm_grad_weights<256><<<weight_blocks, 256, 0, s>>>(d.C, sums, rows, dgamma, dbeta);
         return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
     }
-    const int images = std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / d.chunks));
+    const int images = tdc_norm_chunk_images(d);
     float2 *partial = reinterpret_cast<float2 *>(p->partial);
     TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, {
         const int nv = d.C / V, rows = nv < TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
@@ -420,7 +430,15 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
         const dim3 grid(d.chunks, images);
         if (whole) tdc_norm_grad_sums<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
         else tdc_norm_grad_sums<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
-        tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks + weight_blocks, TDC_NORM_THREADS, d.G * sizeof(float2), s>>>(d, q, out, partial, sums, images * d.chunks, dgamma, dbeta);
+        const size_t lds_means = d.G * sizeof(float2);
+        if (d.chunks > TDC_NORM_PARTS) {
+            float2 *all = reinterpret_cast<float2 *>(p->whole);
+            const unsigned wgs = (unsigned)(((size_t)d.B * d.G + 3) / 4);
+            tdc_norm_grad_combine<<<wgs + weight_blocks, 256, 0, s>>>(d, partial, all, (int)wgs, sums, images * d.chunks, dgamma, dbeta);
+            tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks, TDC_NORM_THREADS, lds_means, s>>>(d, q, out, all, 1, nullptr, 0, nullptr, nullptr);
+        } else {
+            tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks + weight_blocks, TDC_NORM_THREADS, lds_means, s>>>(d, q, out, partial, d.chunks, sums, images * d.chunks, dgamma, dbeta);
+        }
     }));
     return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }

@@ -16,9 +16,12 @@
 
 #include "tdc_typed.h"
 
-constexpr int TDC_NORM_THREADS = 1024;   // of the kernels that run over chunks
+constexpr int TDC_NORM_THREADS = 512;    // of the kernels that run over chunks
 constexpr int TDC_NORM_MAX_C = 8192;     // per-channel pairs of a workgroup fill at most 64 KiB of LDS
 constexpr int TDC_NORM_UNROLL = 4;       // pixels that a thread has in flight
+// Chunks of an image that every workgroup of the second kernel combines for itself.  More than that are combined by a kernel in
+// between: 224x224x64 in fp16, 392 chunks, 36.7 us without it and 13.5 with it.
+constexpr int TDC_NORM_PARTS = 32;
 
 struct TdcNormDims {
     int B, P, C, G, Cg;     // P pixels to an image, Cg channels to a group
@@ -31,12 +34,20 @@ struct tdc_norm_plan {
     TdcNormDims dims;
     int device;
     float4 *partial;     // [B][chunks][G]: number of values, their mean, sum of squares about it; backward: sums of g and g xhat
-    float2 *sums;        // [min(B chunks, TDC_NORM_SUM_ROWS)][C]: backward, sums of d and d xhat over some images or chunks
+    float4 *whole;       // [B][G]: the same of an image
+    float2 *sums;        // [tdc_norm_sum_rows][C]: backward, sums of d and d xhat over some images or chunks
     size_t ws_bytes;
 };
 
-// Workgroups to a channel in the backward pass, at most: as many rows of sums are left to add up for dgamma and dbeta.
+// Backward, the workgroups to a channel leave a row of sums each, to be added up for dgamma and dbeta: some 512 rows.  Resident,
+// every row is of some images; over chunks, there are as many rows to every chunk as this many images at a time make.
 constexpr int TDC_NORM_SUM_ROWS = 512;
+inline int tdc_norm_resident_rows(const TdcNormDims &d, int slices) { return std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / slices)); }
+inline int tdc_norm_chunk_images(const TdcNormDims &d) { return std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / d.chunks)); }
+inline size_t tdc_norm_sum_rows(const TdcNormDims &d)
+{
+    return std::max<size_t>((size_t)tdc_norm_chunk_images(d) * d.chunks, tdc_norm_resident_rows(d, 1));
+}
 
 // Pixels of chunk i of an image.
 __host__ __device__ inline int tdc_chunk_len(const TdcNormDims &d, int i)
@@ -282,15 +293,16 @@ template <int I, int THREADS> __device__ __forceinline__ int tdc_norm_put_sums(f
     return rows;
 }
 
-// The chunks' sums of image b as {mean, rstd} of every group into `stats` [G] in LDS.  Every thread of the workgroup calls it.
-__device__ __forceinline__ void tdc_combine_chunks(const TdcNormDims &d, const float4 *partial, int b, float2 *stats, int threads)
+// `parts` sums of image b combined group by group: f(g, values, mean, squares about it) in one lane of a group's team.
+template <typename F> __device__ __forceinline__ void tdc_combine(const TdcNormDims &d, const float4 *partial, int parts, int b, int threads, F f)
 {
-    const int L = tdc_team(d.G, d.chunks, threads), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = threads / L;
+    const int L = tdc_team(d.G, parts, threads), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = threads / L;
     for (int g0 = 0; g0 < d.G; g0 += teams) {
         const int g = min(g0 + team, d.G - 1);
-        const float4 *p = partial + (size_t)b * d.chunks * d.G + g;
+        const float4 *p = partial + (size_t)b * parts * d.G + g;
         float n = 0.f, s = 0.f;
-        for (int i = lane; i < d.chunks; i += L) {
+#pragma unroll 4
+        for (int i = lane; i < parts; i += L) {
             const float4 o = p[(size_t)i * d.G];
             n += o.x;
             s += o.x * o.y;
@@ -298,14 +310,34 @@ __device__ __forceinline__ void tdc_combine_chunks(const TdcNormDims &d, const f
         n = tdc_lane_sum(n, L);
         const float mean = tdc_lane_sum(s, L) / n;
         float m2 = 0.f;
-        for (int i = lane; i < d.chunks; i += L) {
+#pragma unroll 4
+        for (int i = lane; i < parts; i += L) {
             const float4 o = p[(size_t)i * d.G];
             m2 += o.z + o.x * (o.y - mean) * (o.y - mean);
         }
         m2 = tdc_lane_sum(m2, L);
-        if (lane == 0 && g0 + team < d.G) stats[g] = make_float2(mean, tdc_rstd(m2 / n, d.eps));
+        if (lane == 0 && g0 + team < d.G) f(g, n, mean, m2);
     }
-    __syncthreads();
+}
+
+// The same for plain sums: f(g, first sum, second sum).
+template <typename F> __device__ __forceinline__ void tdc_combine_sums(const TdcNormDims &d, const float2 *partial, int parts, int b, int threads, F f)
+{
+    const int L = tdc_team(d.G, parts, threads), lane = threadIdx.x & (L - 1), team = threadIdx.x / L, teams = threads / L;
+    for (int g0 = 0; g0 < d.G; g0 += teams) {
+        const int g = min(g0 + team, d.G - 1);
+        const float2 *p = partial + (size_t)b * parts * d.G + g;
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll 4
+        for (int i = lane; i < parts; i += L) {
+            const float2 o = p[(size_t)i * d.G];
+            s1 += o.x;
+            s2 += o.y;
+        }
+        s1 = tdc_lane_sum(s1, L);
+        s2 = tdc_lane_sum(s2, L);
+        if (lane == 0 && g0 + team < d.G) f(g, s1, s2);
+    }
 }
 
 // The most neighbours that one access may take: V elements, at most 16 bytes, a power of two.
@@ -323,8 +355,8 @@ inline int tdc_norm_vec(int dtype, int C, std::initializer_list<int64_t> pitches
 
 // ---- the resident form
 
-// Pieces of x that a thread holds at most.  Forward, 1024 threads have 128 registers each: 64 values of fp32, 32 of 16 bits that
-// have to be converted.  Backward, where d is held too, in fp32, 512 threads have 256.
+// Pieces of x that a thread holds at most.  Forward, two workgroups of 512 threads to a compute unit have 128 registers a thread:
+// 64 values of fp32, 32 of 16 bits that have to be converted.  Backward, where d is held too, in fp32, it is one with 256.
 __host__ __device__ constexpr int tdc_norm_held(int V, int size, bool backward) { return backward ? 8 : (V >= 4 && size == 2 ? 8 : 16); }
 
 // A workgroup takes `width` channels, whole groups and whole pieces, of an image; `slices` of them to an image.
@@ -332,38 +364,38 @@ struct TdcNormSlice {
     int width, slices, threads, held;    // held: pieces to a thread; 0: the image does not fit
 };
 
-// Slices are lines of 128 bytes where a workgroup's registers hold that much, and else less, down to one group.  A line that two or four workgroups share comes from memory once all the
-// same: they run on the same XCD (tdc_norm_place).
+// The narrowest slices (whole groups, whole pieces, multiples of `multiple`) are widened to 64 bytes of a pixel, and until there
+// are no more than 1024 of them, as long as 512 threads hold them and 256 workgroups are left.  A line that several workgroups
+// share comes from memory once all the same: they run on the same XCD (tdc_norm_place).  Measured, forward, fp32, 28x28x512, 32
+// images: 16 channels 20.4 us, 32 20.0, 64 22.5; 28x28x128 in bf16: 8 channels 12.4, 16 9.9, 32 11.6; 7x7x512, 256 images: 16
+// channels 25 us, 64 18, 128 16.4.  1024 threads lose everywhere (no second workgroup that reads while one writes) but where
+// slices below 64 bytes of a tensor larger than the L2s can be wider by them: 56x56x256, 32 images: 8 channels 42.4 us, 16 40.2.
 inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool backward, int multiple)
 {
+    const int most = tdc_norm_held(V, tdc_dtype_bytes(dtype), backward), size = tdc_dtype_bytes(dtype);
     int unit = d.Cg;
-    while (unit % V || unit % multiple) {
-        unit += d.Cg;
-        if (unit >= d.C) break;
-    }
+    while ((unit % V || unit % multiple) && unit < d.C) unit += d.Cg;
     if (unit > d.C || d.C % unit) unit = d.C;
-    auto fits = [&](int width, int threads) {
+    auto held = [&](int width, int threads) {
         const int nv = width / V;
         return nv <= threads && width / d.Cg <= threads ? (d.P + threads / nv - 1) / (threads / nv) : 1 << 30;
     };
-    const int most = tdc_norm_held(V, tdc_dtype_bytes(dtype), backward);
-    TdcNormSlice best{0, 0, 0, 0};
-    for (int width = unit; width <= d.C; width += unit) {
-        if (d.C % width) continue;
-        const int line = width * tdc_dtype_bytes(dtype);
-        if (best.held && line > 128) break;
-        for (int threads : {256, 512, 1024}) {
-            const int held = fits(width, threads), top = backward ? 512 : 1024;
-            if (held > most || threads > top) continue;
-            if (held > 4 && threads < top) continue;    // rather more threads than more to each
-            best = TdcNormSlice{width, d.C / width, threads, held};
-            break;
-        }
-        if (best.width != width) break;                 // wider ones fit even less
-        // few images: as many workgroups as can be, for the one wave of them that there is
-        if ((int64_t)d.B * (d.C / width) <= 512) break;
+    auto next = [&](int width) {
+        do width += unit;
+        while (width < d.C && d.C % width);
+        return width;
+    };
+    auto fits = [&](int width) { return held(width, 512) <= most; };
+    auto groups = [&](int width) { return (int64_t)d.B * (d.C / width); };
+    if (!fits(unit)) return TdcNormSlice{0, 0, 0, 0};
+    int width = unit;
+    for (int w = next(width); w <= d.C && (width * size < 64 || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
+    if (!backward && width * size < 64 && (int64_t)d.B * d.P * d.C * size > (32 << 20)) {
+        const int w = next(width);
+        if (w <= d.C && held(w, 1024) <= most) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
     }
-    return best;
+    const int threads = held(width, 256) <= 4 ? 256 : 512;
+    return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
 }
 
 // Workgroup id -> (image, slice): the ids that one XCD gets, 8 apart, are neighbours.
@@ -375,14 +407,15 @@ __device__ __forceinline__ void tdc_norm_place(int id, int total, int slices, in
     slice = t - b * slices;
 }
 
-// The statements with the constants THREADS and HELD that a slice asks for; TOP is the most threads, MOST what tdc_norm_held says.
-#define TDC_FOR_SLICE(s, TOP, MOST, THREADS, HELD, ...)                                                                             \
+// The statements with the constants THREADS and HELD that a slice asks for; MOST is what tdc_norm_held says, FORWARD what it was
+// told.
+#define TDC_FOR_SLICE(s, MOST, FORWARD, THREADS, HELD, ...)                                                                         \
     do {                                                                                                                            \
         if ((s).threads == 256) { constexpr int THREADS = 256, HELD = 4; __VA_ARGS__; }                                             \
-        else if ((s).threads == 512 && (s).held <= 4) { constexpr int THREADS = 512, HELD = 4; __VA_ARGS__; }                       \
-        else if ((s).held <= 4) { if constexpr ((TOP) == 1024) { constexpr int THREADS = 1024, HELD = 4; __VA_ARGS__; } }           \
-        else if ((s).held <= 8) { constexpr int THREADS = TOP, HELD = 8; __VA_ARGS__; }                                             \
-        else if constexpr ((MOST) >= 16) { constexpr int THREADS = TOP, HELD = 16; __VA_ARGS__; }                                   \
+        else if ((s).threads == 1024) { if constexpr (FORWARD) { constexpr int THREADS = 1024, HELD = MOST; __VA_ARGS__; } }        \
+        else if ((s).held <= 4) { constexpr int THREADS = 512, HELD = 4; __VA_ARGS__; }                                             \
+        else if ((s).held <= 8) { constexpr int THREADS = 512, HELD = 8; __VA_ARGS__; }                                             \
+        else if constexpr ((MOST) >= 16) { constexpr int THREADS = 512, HELD = 16; __VA_ARGS__; }                                   \
     } while (0)
 
 #endif  // TDC_NORM_INTERNAL_H

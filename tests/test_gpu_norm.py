@@ -49,7 +49,9 @@ def _check_forward(y, x, G, act, dtype, gamma, beta, res, what, eps=EPS):
 
 # B, H, W, C, groups: one value, one pixel, one channel to a group, one group, odd everything, more channels than threads, long images
 SHAPES = [(1, 1, 1, 1, 1), (2, 1, 1, 64, 8), (5, 1, 1, 24, 24), (3, 7, 7, 32, 32), (2, 9, 5, 48, 1), (3, 5, 7, 150, 10), (2, 3, 3, 2048, 32), (1, 4, 4, 8192, 8),
-          (2, 6, 5, 1236, 3), (1, 31, 33, 7, 7), (2, 56, 56, 64, 32), (1, 150, 201, 16, 4), (40, 3, 2, 36, 6), (1, 1, 4099, 8, 2), (3, 14, 14, 1022, 2)]
+          (2, 6, 5, 1236, 3), (1, 31, 33, 7, 7), (2, 56, 56, 64, 32), (1, 150, 201, 16, 4), (40, 3, 2, 36, 6), (1, 1, 4099, 8, 2), (3, 14, 14, 1022, 2),
+          # one image in over 512 parts; many images of a pixel; many of several parts each
+          (1, 224, 224, 64, 32), (700, 1, 1, 64, 4), (70, 40, 40, 12, 1)]
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["fp32", "fp16", "bf16"])
