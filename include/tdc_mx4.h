@@ -10,7 +10,8 @@
  * that holds an infinity or a NaN gets e = 255.  The result is exact: it depends on nothing but the values.
  *
  * Products sum in fp32 on the matrix cores that multiply such blocks directly.  As in tdc.h the calls only enqueue work on
- * `hip_stream`, allocate nothing and may be captured; codes must be 16-byte aligned, the other pointers to their elements.
+ * `hip_stream`, allocate nothing and may be captured; codes must be 16-byte aligned, the other pointers to their elements.  Rows
+ * may have up to 2^30 values.
  * Outputs must not overlap inputs.  Calls without a plan run on the calling thread's CURRENT device, which must be the
  * stream's and the tensors'.
  */

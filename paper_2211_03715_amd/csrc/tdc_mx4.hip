@@ -123,7 +123,9 @@ struct tdc_mx4_plan {
     int device;
     int64_t rows;            // output pixels
     TdcMx4Rows map;          // output pixel -> input pixel
-    uint8_t *w_codes, *w_scales, *x_codes, *x_scales;
+    uint8_t *w_codes, *w_scales, *x_codes, *x_scales;   // plain: for large products, and what the others are laid out from
+    uint8_t *w_laid, *ws_laid;                          // as tdc_mx4_rows.hip takes them
+    bool large;                                         // runs as a large product
     bool packed;
     size_t ws_bytes;
 };
@@ -136,7 +138,7 @@ int tdc_mx4_quantize(void *hip_stream, const void *x, int dtype, int64_t rows, i
     if (!x || !codes || !scales) return TDC_ERR_NULL;
     if (pitch == 0) pitch = cols;
     if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
-    if (!tdc_known_dtype(dtype) || cols > 0x7fffffff - 31 || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(x, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(x, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     if (rows > INT64_MAX / 64 / tdc_mx4_blocks((int)cols) || !blocks_for(rows * tdc_mx4_blocks((int)cols), 256)) return TDC_ERR_UNSUPPORTED;
     return launch_quantize((hipStream_t)hip_stream, x, dtype, TdcMx4Rows::all(), rows, (int)cols, pitch, codes, scales) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
@@ -147,7 +149,7 @@ int tdc_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint8_t *sc
     if (!y || !codes || !scales) return TDC_ERR_NULL;
     if (pitch == 0) pitch = cols;
     if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
-    if (!tdc_known_dtype(dtype) || cols > 0x7fffffff - 31 || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     const int nb = tdc_mx4_blocks((int)cols);
     if (rows > INT64_MAX / 64 / nb) return TDC_ERR_UNSUPPORTED;
     const int64_t total = rows * nb * 4;
@@ -169,7 +171,7 @@ int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_sc
     if (!a_codes || !a_scales || !b_codes || !b_scales || !y) return TDC_ERR_NULL;
     const int rc = check_epilogue(epilogue, dtype);
     if (rc != TDC_OK) return rc;
-    if (K > 0x7fffffff - 31 || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (K > TDC_MX4_MAX_COLS || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     if (!tdc_mx4_product_fits(M, N)) return TDC_ERR_UNSUPPORTED;
     const TdcMx4Product q{a_codes, a_scales, b_codes, b_scales, M, N, tdc_mx4_blocks(K), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
@@ -184,7 +186,7 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     if (s.x_pitch == 0) s.x_pitch = s.C;
     if (s.x_pitch < s.C) return TDC_ERR_BAD_SHAPE;
     const int64_t Ho = (s.H - 1) / s.stride + 1, Wo = (s.W - 1) / s.stride + 1, lim = 0x7fffffff;
-    if (!tdc_known_dtype(s.dtype) || s.C > lim - 31) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS) return TDC_ERR_UNSUPPORTED;
     if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
     const int64_t rows = s.batch * Ho * Wo;
     if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 256)) return TDC_ERR_UNSUPPORTED;
@@ -200,8 +202,10 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     p->map = s.stride == 1 ? TdcMx4Rows::all() : TdcMx4Rows{s.stride, (int)Wo, (int)(Ho * Wo), s.W, s.H * s.W};
     const size_t nb = tdc_mx4_blocks(s.C);
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    const size_t parts[4] = {up(s.N * nb * 16), up(s.N * nb), up(rows * nb * 16), up(rows * nb)};
-    p->ws_bytes = parts[0] + parts[1] + parts[2] + parts[3];
+    p->large = tdc_mx4_large(rows, s.N, s.C);
+    const size_t parts[6] = {up(s.N * nb * 16), up(s.N * nb), p->large ? up(rows * nb * 16) : 0, p->large ? up(rows * nb) : 0,
+                             p->large ? 0 : tdc_mx4_laid_out_bytes(s.N, (int)nb), p->large ? 0 : tdc_mx4_laid_out_scale_bytes(s.N, (int)nb)};
+    for (size_t n : parts) p->ws_bytes += n;
     if (hipMalloc((void **)&p->w_codes, p->ws_bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete p;
@@ -210,6 +214,20 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     p->w_scales = p->w_codes + parts[0];
     p->x_codes = p->w_scales + parts[1];
     p->x_scales = p->x_codes + parts[2];
+    p->w_laid = p->x_scales + parts[3];
+    p->ws_laid = p->w_laid + parts[4];
+    if (!p->large) {
+        // whatever a first launch would have to set up, now: a convolution may be the first thing a capturing stream sees
+        const TdcMx4Product q{nullptr, nullptr, nullptr, nullptr, (int)rows, s.N, (int)nb, p->map, nullptr, kernel_epilogue(nullptr), false};
+        for (int kind = 0; kind < 3; ++kind) {   // x quantised, in pieces of 16 bytes, one value at a time
+            const TdcMx4Source src{kind == 0 ? nullptr : (const char *)nullptr + (kind == 1 ? 16 : 2), s.x_pitch, s.C};
+            if (tdc_launch_mx4_rows(q, src, s.dtype, p->w_laid, p->ws_laid, nullptr, true) != hipSuccess) {
+                (void)hipGetLastError();
+                tdc_mx4_plan_destroy(p);
+                return TDC_ERR_HIP;
+            }
+        }
+    }
     *out = p;
     return TDC_OK;
 }
@@ -225,7 +243,7 @@ int tdc_mx4_plan_destroy(tdc_mx4_plan *p)
 
 size_t tdc_mx4_plan_workspace_bytes(const tdc_mx4_plan *p) { return p ? p->ws_bytes : 0; }
 
-int tdc_mx4_plan_kernel_count(const tdc_mx4_plan *p) { return p ? 2 : 0; }
+int tdc_mx4_plan_kernel_count(const tdc_mx4_plan *p) { return !p ? 0 : p->large ? 2 : 1; }
 
 int tdc_mx4_plan_pack(tdc_mx4_plan *p, void *hip_stream, const float *W)
 {
@@ -237,6 +255,7 @@ int tdc_mx4_plan_pack(tdc_mx4_plan *p, void *hip_stream, const float *W)
     const dim3 grid((N + 255) / 256, nb < 65535 ? nb : 65535);
     tdc_mx4_pack_weights<<<grid, 256, 0, (hipStream_t)hip_stream>>>(W, C, N, nb, p->w_codes, p->w_scales);
     if (hipGetLastError() != hipSuccess) return TDC_ERR_HIP;
+    if (!p->large && tdc_launch_mx4_lay_out(p->w_codes, p->w_scales, N, nb, p->w_laid, p->ws_laid, (hipStream_t)hip_stream) != hipSuccess) return TDC_ERR_HIP;
     p->packed = true;
     return TDC_OK;
 }
@@ -251,6 +270,10 @@ int tdc_conv_mx4(tdc_mx4_plan *p, void *hip_stream, const void *x, void *y, cons
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (!p->large) {
+        const TdcMx4Product q{nullptr, nullptr, nullptr, nullptr, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue), false};
+        return tdc_launch_mx4_rows(q, TdcMx4Source{x, s.x_pitch, s.C}, s.dtype, p->w_laid, p->ws_laid, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    }
     if (launch_quantize(st, x, s.dtype, p->map, p->rows, s.C, s.x_pitch, p->x_codes, p->x_scales) != hipSuccess) return TDC_ERR_HIP;
     const TdcMx4Product q{p->x_codes, p->x_scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, s.dtype, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
@@ -266,6 +289,7 @@ int tdc_conv_mx4_quantized(tdc_mx4_plan *p, void *hip_stream, const uint8_t *cod
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
     const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue), false};
+    if (!p->large) return tdc_launch_mx4_rows(q, TdcMx4Source{nullptr, 0, 0}, s.dtype, p->w_laid, p->ws_laid, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
     return tdc_launch_mx4_product(q, s.dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 

@@ -42,4 +42,24 @@ inline bool tdc_mx4_product_fits(int64_t M, int64_t N) { return ((M + 31) / 32) 
 
 hipError_t tdc_launch_mx4_product(const TdcMx4Product &q, int dtype, hipStream_t s);
 
+// Rows of A in floating point, quantised on the way (a_codes, a_scales unused), or x null.
+struct TdcMx4Source {
+    const void *x;
+    int64_t pitch;
+    int cols;
+};
+
+// Weights as tdc_mx4_rows.hip takes them.
+size_t tdc_mx4_laid_out_bytes(int N, int nb);
+size_t tdc_mx4_laid_out_scale_bytes(int N, int nb);
+hipError_t tdc_launch_mx4_lay_out(const uint8_t *codes, const uint8_t *scales, int N, int nb, uint8_t *w, uint8_t *ws, hipStream_t s);
+// The product with laid-out weights, or, w and ws null, with q's own second operand.  prepare_only: what must precede a first
+// launch, without one.
+hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, int dtype, const uint8_t *w, const uint8_t *ws, hipStream_t s, bool prepare_only = false);
+
+constexpr int TDC_MX4_MAX_COLS = 1 << 30;
+
+// A convolution that the matrix cores bound rather than memory runs as quantisation and a product in large tiles.
+inline bool tdc_mx4_large(int64_t rows, int N, int K) { return rows >= 4096 && N >= 1024 && K >= 1024; }
+
 #endif  // TDC_MX4_INTERNAL_H

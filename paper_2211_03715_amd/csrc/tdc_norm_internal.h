@@ -20,8 +20,8 @@ constexpr int TDC_NORM_THREADS = 512;    // of the kernels that run over chunks
 constexpr int TDC_NORM_MAX_C = 8192;     // per-channel pairs of a workgroup fill at most 64 KiB of LDS
 constexpr int TDC_NORM_UNROLL = 4;       // pixels that a thread has in flight
 // Chunks of an image that every workgroup of the second kernel combines for itself.  More than that are combined by a kernel in
-// between: 224x224x64 in fp16, 392 chunks, 36.7 us without it and 13.5 with it.
-constexpr int TDC_NORM_PARTS = 32;
+// between: 224x224x64 in fp16, 196 chunks, 18.2 us without it and 16.1 with it; at 64 chunks the two are even.
+constexpr int TDC_NORM_PARTS = 64;
 
 struct TdcNormDims {
     int B, P, C, G, Cg;     // P pixels to an image, Cg channels to a group
@@ -116,17 +116,6 @@ template <int V, bool WHOLE> struct TdcNormSums {
         if (k == U) add_some<true>(in, U);
         else add_some<false>(in, k);
     }
-    __device__ __forceinline__ void merge(float n_b, const float (&mean_b)[I], const float (&m2_b)[I])
-    {
-        const float tot = n + n_b, w = tot > 0.f ? n_b * __builtin_amdgcn_rcpf(tot) : 0.f;
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const float off = mean_b[i] - mean[i];
-            mean[i] += off * w;
-            m2[i] += m2_b[i] + off * off * (n * w);
-        }
-        n = tot;
-    }
 };
 
 // Items in LDS: `rows` rows of nv pieces, with the values that an item of the row stands for.  Where nv is a power of two below
@@ -158,19 +147,29 @@ __device__ __forceinline__ int tdc_norm_put(const TdcNormItems &to, TdcNormSums<
     int row = t.r, rows = used;
     bool writes = live;
     if (tdc_norm_by_wave(nv)) {
-        tdc_merge_lanes(nv, [&](auto first, auto second) {
-            float mean[I], m2[I];
-            const float n = second(s.n);
-            s.n = first(s.n);
+        // first the mean of the lanes that belong together, then the squares about that: plain sums both
+        const float n = s.n;
+        float sum[I], m2[I];
 #pragma unroll
-            for (int i = 0; i < I; ++i) {
-                mean[i] = second(s.mean[i]);
-                m2[i] = second(s.m2[i]);
-                s.mean[i] = first(s.mean[i]);
-                s.m2[i] = first(s.m2[i]);
-            }
-            s.merge(n, mean, m2);
+        for (int i = 0; i < I; ++i) sum[i] = n * s.mean[i];
+        tdc_merge_lanes(nv, [&](auto first, auto second) {
+            s.n = first(s.n) + second(s.n);
+#pragma unroll
+            for (int i = 0; i < I; ++i) sum[i] = first(sum[i]) + second(sum[i]);
         });
+        const float inv = s.n > 0.f ? 1.f / s.n : 0.f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const float mean = sum[i] * inv, off = s.mean[i] - mean;
+            m2[i] = s.m2[i] + n * off * off;
+            s.mean[i] = mean;
+        }
+        tdc_merge_lanes(nv, [&](auto first, auto second) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) m2[i] = first(m2[i]) + second(m2[i]);
+        });
+#pragma unroll
+        for (int i = 0; i < I; ++i) s.m2[i] = m2[i];
         row = threadIdx.x / 64;
         rows = THREADS / 64;
         writes = (threadIdx.x & 63) < nv;
