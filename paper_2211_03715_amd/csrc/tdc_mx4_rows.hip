@@ -1,7 +1,7 @@
 // Products with one operand kept whole in LDS (tdc_mx4.h): 1x1 convolutions, which are bound by reading x and writing y, and
 // products of few rows, which are bound by reading the weights and by latency.
 //
-// A workgroup takes 32 RB rows.  It quantises them on the way into LDS (or takes them quantised), all of k where that fits, and
+// A workgroup takes 32 rows.  It quantises them on the way into LDS (or takes them quantised), all of k where that fits, and
 // multiplies them with 64 columns of weights at a time: x is read once, y written once, in one launch; the weights come from the
 // L2.  KW = 1: its four wavefronts take columns in turn.  KW = 8: eight wavefronts share the k of the same 64 columns and add up
 // through LDS, so that few rows still keep many wavefronts reading weights.
@@ -57,28 +57,66 @@ template <typename T, int SRC> __device__ __forceinline__ void load8(const T *ro
     }
 }
 
-// Sums of columns n and n + 1 of row m.
-template <typename T> __device__ __forceinline__ void finish_pair(const RowsArgs &a, float v0, float v1, int m, int n)
+// The epilogue of a lane's columns n and n + 1: sums s of E rows, row(e) + 4 h from m0 on.  row(e) is the same for all lanes, so
+// that a row's address is a scalar one, and the lane adds the same 32-bit offset to all of them.  What is read for some rows is
+// read before any of them is stored: a store might change it, for all the compiler knows.
+template <typename T, int E, typename Row> __device__ __forceinline__ void finish_columns(const RowsArgs &a, int m0, int rows, int n, int h, Row row, float (&s)[E][2])
 {
-    if (a.pairs) {
-        if (n < a.q.N) {
-            float v[2] = {v0, v1};
-            tdc_mx4_finish<T, 2>(a.q, v, m, n);
+    if (n >= a.q.N) return;
+    const bool two = n + 1 < a.q.N;
+    const unsigned lane = ((unsigned)(4 * h) * a.q.N + n) * sizeof(T);
+    if (a.q.epi.bias) {
+        const float b0 = a.q.epi.bias[n], b1 = two ? a.q.epi.bias[n + 1] : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            s[e][0] += b0;
+            s[e][1] += b1;
         }
-    } else {
-        float u[1] = {v0}, w[1] = {v1};
-        if (n < a.q.N) tdc_mx4_finish<T, 1>(a.q, u, m, n);
-        if (n + 1 < a.q.N) tdc_mx4_finish<T, 1>(a.q, w, m, n + 1);
+    }
+    if (a.q.epi.residual) {
+        float r[E][2];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (row(e) + 4 * h >= rows) continue;
+            const T *p = reinterpret_cast<const T *>(static_cast<const char *>(a.q.epi.residual) + (size_t)(m0 + row(e)) * a.q.N * sizeof(T) + lane);
+            if (a.pairs) {
+                const TdcVec<T, 2> v = tdc_load<T, 2>(p);
+                r[e][0] = (float)v.v[0];
+                r[e][1] = (float)v.v[1];
+            } else {
+                r[e][0] = (float)p[0];
+                r[e][1] = two ? (float)p[1] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (row(e) + 4 * h < rows) {
+                s[e][0] += r[e][0];
+                s[e][1] += r[e][1];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) tdc_activate_all(a.q.epi.act, s[e]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (row(e) + 4 * h >= rows) continue;
+        T *p = reinterpret_cast<T *>(static_cast<char *>(a.q.y) + (size_t)(m0 + row(e)) * a.q.N * sizeof(T) + lane);
+        if (a.pairs) {
+            tdc_store<T, 2>(p, s[e]);
+        } else {
+            p[0] = (T)s[e][0];
+            if (two) p[1] = (T)s[e][1];
+        }
     }
 }
 
-template <typename T, int RB, int SRC, int KW, bool PLAIN>
-__global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
+template <typename T, int SRC, int KW, bool PLAIN>
+__global__ __launch_bounds__(KW == 1 ? 256 : 512, 4) void tdc_mx4_rows(RowsArgs a)
 {
-    constexpr int THREADS = KW == 1 ? 256 : 512, ROWS = 32 * RB;
+    constexpr int THREADS = KW == 1 ? 256 : 512, ROWS = 32;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    // codes [4 chunk][RB][64 lanes][16], scales [chunk][RB][64 lanes][4]
-    uint8_t *const codes = lds, *const scales = lds + (size_t)a.chunk * 4 * RB * 1024;
+    // codes [4 chunk][64 lanes][16], scales [chunk][64 lanes][4]
+    uint8_t *const codes = lds, *const scales = lds + (size_t)a.chunk * 4096;
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = l & 31, h = l >> 5;
     const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, m0 = tile * ROWS, rows = min(ROWS, a.q.M - m0);
 
@@ -115,8 +153,8 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
                     sc[u] = tdc_mx4_scale(tdc_lane_max<4>(top));         // four neighbouring lanes have a block
                 }
                 if (i0 + u * THREADS >= total) break;
-                const int s = kb[u] >> 1, lane = (kb[u] & 1) * 32 + (row[u] & 31), rb = row[u] >> 5;
-                uint8_t *to = codes + ((size_t)(s * RB + rb) * 64 + lane) * 16, *sto = scales + (((s >> 2) * RB + rb) * 64 + lane) * 4 + (s & 3);
+                const int s = kb[u] >> 1, lane = (kb[u] & 1) * 32 + row[u];
+                uint8_t *to = codes + s * 1024 + lane * 16, *sto = scales + (s >> 2) * 256 + lane * 4 + (s & 3);
                 if constexpr (SRC == SRC_CODES) {
                     *reinterpret_cast<tdc_i4 *>(to) = c[u];
                     *sto = (uint8_t)sc[u];
@@ -128,10 +166,10 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
         }
     };
 
-    // 256 values of k, quad `t` of the weights and `at` in LDS, of columns 64 p ..
-    auto multiply = [&](int p, int t, int at, tdc_f16v (&acc)[RB][2]) {
-        tdc_i4 b[4][2];
-        unsigned sb[2];
+    // 256 values of k of columns 64 p ..: the weights of quad t, and their product with what lies at quad `at` in LDS
+    tdc_i4 b[4][2];
+    unsigned sb[2];
+    auto load = [&](int p, int t) {
         if constexpr (PLAIN) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -155,38 +193,35 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
             sb[0] = v.x;
             sb[1] = v.y;
         }
+    };
+    auto multiply = [&](int at, tdc_f16v (&acc)[2]) {
+        const unsigned sa = *reinterpret_cast<const unsigned *>(scales + at * 256 + l * 4);
+        tdc_i4 x[4];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) {
-            const unsigned sa = *reinterpret_cast<const unsigned *>(scales + ((at * RB + i) * 64 + l) * 4);
-            tdc_i4 x[4];
+        for (int s = 0; s < 4; ++s) x[s] = *reinterpret_cast<const tdc_i4 *>(codes + (4 * at + s) * 1024 + l * 16);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) x[s] = *reinterpret_cast<const tdc_i4 *>(codes + ((size_t)((4 * at + s) * RB + i) * 64 + l) * 16);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = tdc_mx4_mfma<0>(x[0], sa, b[0][j], sb[j], acc[i][j]);
-                acc[i][j] = tdc_mx4_mfma<1>(x[1], sa, b[1][j], sb[j], acc[i][j]);
-                acc[i][j] = tdc_mx4_mfma<2>(x[2], sa, b[2][j], sb[j], acc[i][j]);
-                acc[i][j] = tdc_mx4_mfma<3>(x[3], sa, b[3][j], sb[j], acc[i][j]);
-            }
+        for (int j = 0; j < 2; ++j) {
+            acc[j] = tdc_mx4_mfma<0>(x[0], sa, b[0][j], sb[j], acc[j]);
+            acc[j] = tdc_mx4_mfma<1>(x[1], sa, b[1][j], sb[j], acc[j]);
+            acc[j] = tdc_mx4_mfma<2>(x[2], sa, b[2][j], sb[j], acc[j]);
+            acc[j] = tdc_mx4_mfma<3>(x[3], sa, b[3][j], sb[j], acc[j]);
         }
     };
 
+    const int first = (int)((int64_t)a.groups * split / a.splits), end = (int)((int64_t)a.groups * (split + 1) / a.splits);
     const bool once = a.chunk >= a.quads;
     if (once) {
         stage(0);
         __syncthreads();
     }
-    const int first = (int)((int64_t)a.groups * split / a.splits), end = (int)((int64_t)a.groups * (split + 1) / a.splits);
     for (int p0 = first; p0 < end; p0 += KW == 1 ? 4 : 1) {   // the same trip count for every wavefront
         const int p = KW == 1 ? p0 + wave : p0;
         const bool mine = p < end;
-        tdc_f16v acc[RB][2];
+        tdc_f16v acc[2];
 #pragma unroll
-        for (int i = 0; i < RB; ++i)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+            for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
         for (int quad0 = 0; quad0 < a.quads; quad0 += a.chunk) {
             if (!once) {
                 __syncthreads();
@@ -194,18 +229,23 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
                 __syncthreads();
             }
             const int quads = min(a.chunk, a.quads - quad0);
+            // No fetch ahead: the registers for it cost a wavefront in four, which hides more (56x56x256 -> 512, every second pixel,
+            // 32 images: 19.3 us without, 23.5 with).
             if (mine)
-                for (int t = KW == 1 ? 0 : wave; t < quads; t += KW) multiply(p, quad0 + t, t, acc);
+                for (int t = KW == 1 ? 0 : wave; t < quads; t += KW) {
+                    load(p, quad0 + t);
+                    multiply(t, acc);
+                }
         }
         if constexpr (KW == 1) {
             if (mine) {
 #pragma unroll
-                for (int i = 0; i < RB; ++i)
+                for (int e0 = 0; e0 < 16; e0 += 8) {
+                    float v[8][2];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int r = 32 * i + 8 * (e / 4) + 4 * h + e % 4;
-                        if (r < rows) finish_pair<T>(a, acc[i][0][e], acc[i][1][e], m0 + r, 64 * p + 2 * r32);
-                    }
+                    for (int e = 0; e < 8; ++e) v[e][0] = acc[0][e0 + e], v[e][1] = acc[1][e0 + e];
+                    finish_columns<T, 8>(a, m0, rows, 64 * p + 2 * r32, h, [&](int e) { return 8 * ((e0 + e) / 4) + e % 4; }, v);
+                }
             }
         } else {
             // every wavefront's sums through LDS; wavefront w finishes registers 2w and 2w + 1
@@ -214,28 +254,28 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512) void tdc_mx4_rows(RowsArgs a)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sums[((wave * 2 + j) * 16 + e) * 64 + l] = acc[0][j][e];
+                for (int e = 0; e < 16; ++e) sums[((wave * 2 + j) * 16 + e) * 64 + l] = acc[j][e];
             __syncthreads();
+            float v[2][2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int e = 2 * wave + u, r = 8 * (e / 4) + 4 * h + e % 4;
-                float v[2] = {0.f, 0.f};
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < 2; ++j) {
+                    v[u][j] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < KW; ++w) v[j] += sums[((w * 2 + j) * 16 + e) * 64 + l];
-                if (r < rows) finish_pair<T>(a, v[0], v[1], m0 + r, 64 * p + 2 * r32);
-            }
+                    for (int w = 0; w < KW; ++w) v[u][j] += sums[((w * 2 + j) * 16 + 2 * wave + u) * 64 + l];
+                }
+            finish_columns<T, 2>(a, m0, rows, 64 * p + 2 * r32, h, [&](int u) { return 8 * ((2 * wave + u) / 4) + (2 * wave + u) % 4; }, v);
         }
     }
 }
 
-template <typename T, int RB, int SRC, int KW, bool PLAIN> hipError_t launch(const RowsArgs &a, unsigned wgs, size_t lds, hipStream_t s, bool prepare_only)
+template <typename T, int SRC, int KW, bool PLAIN> hipError_t launch(const RowsArgs &a, unsigned wgs, size_t lds, hipStream_t s, bool prepare_only)
 {
-    const void *fn = (const void *)&tdc_mx4_rows<T, RB, SRC, KW, PLAIN>;
+    const void *fn = (const void *)&tdc_mx4_rows<T, SRC, KW, PLAIN>;
     const hipError_t e = tdc_allow_lds(fn, lds);
     if (e != hipSuccess || prepare_only) return e;
-    tdc_mx4_rows<T, RB, SRC, KW, PLAIN><<<wgs, KW == 1 ? 256 : 512, lds, s>>>(a);
+    tdc_mx4_rows<T, SRC, KW, PLAIN><<<wgs, KW == 1 ? 256 : 512, lds, s>>>(a);
     return hipGetLastError();
 }
 
@@ -282,15 +322,13 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
     a.quads = quads_of(q.nb);
     const int size = tdc_dtype_bytes(dtype);
     a.pairs = q.N % 2 == 0 && tdc_aligned_to(q.y, 2 * size) && tdc_aligned_to(q.epi.residual, 2 * size);
-    const int64_t tiles32 = ((int64_t)q.M + 31) / 32;
+    const int64_t tiles = ((int64_t)q.M + 31) / 32;
     // Few tiles: a workgroup to 32 rows and 64 columns, eight wavefronts along k.  Many: the columns in turn, shared by as many
     // workgroups as it takes to have two to a compute unit.
-    const bool few = tiles32 * a.groups <= 512 || !w;
-    const int rb = few ? 1 : 2;
-    const int64_t tiles = ((int64_t)q.M + 32 * rb - 1) / (32 * rb);
+    const bool few = tiles * a.groups <= 512 || !w;
     a.splits = few ? a.groups : (int)std::max<int64_t>(1, std::min<int64_t>((a.groups + 3) / 4, 512 / tiles));
-    // 17 KiB of LDS to 32 rows and 1024 values of k; KW = 8 adds up in 64 KiB
-    const size_t per_quad = (size_t)rb * (4096 + 256);
+    // 4 KiB of codes and 256 bytes of scales to 256 values of k; KW = 8 adds up in 64 KiB
+    constexpr size_t per_quad = 4096 + 256;
     a.chunk = (int)std::min<size_t>(a.quads, 139264 / per_quad);
     a.blocks = tdc_make_div(a.chunk * QUAD_BLOCKS);
     const size_t lds = std::max<size_t>(a.chunk * per_quad, few ? 65536 : 0);
@@ -298,15 +336,15 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
     const bool vectors = src.x && src.cols % 8 == 0 && tdc_aligned_to(src.x, 16) && src.pitch * size % 16 == 0;
     hipError_t e = hipErrorInvalidValue;
     TDC_FOR_DTYPE(dtype, T, {
-        if (!w) e = launch<T, 1, SRC_CODES, 8, true>(a, wgs, lds, s, prepare_only);
+        if (!w) e = launch<T, SRC_CODES, 8, true>(a, wgs, lds, s, prepare_only);
         else if (few) {
-            if (!src.x) e = launch<T, 1, SRC_CODES, 8, false>(a, wgs, lds, s, prepare_only);
-            else if (vectors) e = launch<T, 1, SRC_VECTORS, 8, false>(a, wgs, lds, s, prepare_only);
-            else e = launch<T, 1, SRC_VALUES, 8, false>(a, wgs, lds, s, prepare_only);
+            if (!src.x) e = launch<T, SRC_CODES, 8, false>(a, wgs, lds, s, prepare_only);
+            else if (vectors) e = launch<T, SRC_VECTORS, 8, false>(a, wgs, lds, s, prepare_only);
+            else e = launch<T, SRC_VALUES, 8, false>(a, wgs, lds, s, prepare_only);
         } else {
-            if (!src.x) e = launch<T, 2, SRC_CODES, 1, false>(a, wgs, lds, s, prepare_only);
-            else if (vectors) e = launch<T, 2, SRC_VECTORS, 1, false>(a, wgs, lds, s, prepare_only);
-            else e = launch<T, 2, SRC_VALUES, 1, false>(a, wgs, lds, s, prepare_only);
+            if (!src.x) e = launch<T, SRC_CODES, 1, false>(a, wgs, lds, s, prepare_only);
+            else if (vectors) e = launch<T, SRC_VECTORS, 1, false>(a, wgs, lds, s, prepare_only);
+            else e = launch<T, SRC_VALUES, 1, false>(a, wgs, lds, s, prepare_only);
         }
     });
     return e;
