@@ -34,8 +34,13 @@ struct TdcMx4Product {
     TdcMx4Rows a_rows;
     void *y;
     TdcMx4Epi epi;
-    bool vec;                // y and the residual can be accessed 16 bytes at a time
+    bool vec;                // y, the residual and the bias can be accessed 16 bytes at a time
 };
+
+inline bool tdc_mx4_vec(const TdcMx4Product &q, int dtype)
+{
+    return q.N % (16 / tdc_dtype_bytes(dtype)) == 0 && tdc_aligned_to(q.y, 16) && tdc_aligned_to(q.epi.residual, 16) && tdc_aligned_to(q.epi.bias, 16);
+}
 
 // Whether the kernels' grids cover M x N outputs.
 inline bool tdc_mx4_product_fits(int64_t M, int64_t N) { return ((M + 31) / 32) * ((N + 31) / 32) < 0x7fffffff / 256; }

@@ -47,7 +47,7 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 hipError_t tdc_launch_mx4_product(const TdcMx4Product &given, int dtype, hipStream_t s)
 {
     TdcMx4Product q = given;
-    q.vec = q.N % (16 / tdc_dtype_bytes(dtype)) == 0 && tdc_aligned_to(q.y, 16) && tdc_aligned_to(q.epi.residual, 16);
+    q.vec = tdc_mx4_vec(q, dtype);
     if (q.M <= 64) return tdc_launch_mx4_rows(q, TdcMx4Source{nullptr, 0, 0}, dtype, nullptr, nullptr, s);
     const int64_t large = up(q.M, 256) * up(q.N, 256), small = up(q.M, 128) * up(q.N, 128), tiles = up(q.M, 32) * up(q.N, 32);
     const bool packed = q.nb % 16 == 0 && tdc_aligned_to(q.a_scales, 16) && tdc_aligned_to(q.b_scales, 16);

@@ -34,6 +34,8 @@ struct RowsArgs {
 };
 
 constexpr int QUAD_BLOCKS = 8;    // blocks to 256 values
+constexpr size_t per_quad = 4096 + 256;   // their codes and scales, 32 rows
+constexpr int PITCH = 64 + 8;     // floats to a row of sums: the halves of a wavefront, four rows apart, on different banks
 
 // Eight values of x, zeros past the end.
 template <typename T, int SRC> __device__ __forceinline__ void load8(const T *row, int c0, int cols, float (&v)[8])
@@ -238,13 +240,17 @@ __global__ __launch_bounds__(KW == 1 ? 256 : 512, 4) void tdc_mx4_rows(RowsArgs 
                 }
         }
         if constexpr (KW == 1) {
+            // 16 rows at a time through a piece of LDS of the wavefront's own, so that stores are whole lines of 16 bytes a lane
+            float *sums = reinterpret_cast<float *>(lds + (size_t)a.chunk * per_quad) + wave * 16 * PITCH;
             if (mine) {
 #pragma unroll
                 for (int e0 = 0; e0 < 16; e0 += 8) {
-                    float v[8][2];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e][0] = acc[0][e0 + e], v[e][1] = acc[1][e0 + e];
-                    finish_columns<T, 8>(a, m0, rows, 64 * p + 2 * r32, h, [&](int e) { return 8 * ((e0 + e) / 4) + e % 4; }, v);
+                    for (int e = 0; e < 8; ++e)
+                        *reinterpret_cast<float2 *>(sums + (8 * (e / 4) + 4 * h + e % 4) * PITCH + 2 * r32) = make_float2(acc[0][e0 + e], acc[1][e0 + e]);
+                    __builtin_amdgcn_wave_barrier();
+                    tdc_mx4_store_rows<T>(a.q, sums, PITCH, 16, 64, m0 + 2 * e0, 64 * p, l);
+                    __builtin_amdgcn_wave_barrier();
                 }
             }
         } else {
@@ -321,17 +327,17 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
     a.groups = groups_of(q.N);
     a.quads = quads_of(q.nb);
     const int size = tdc_dtype_bytes(dtype);
+    a.q.vec = tdc_mx4_vec(q, dtype);
     a.pairs = q.N % 2 == 0 && tdc_aligned_to(q.y, 2 * size) && tdc_aligned_to(q.epi.residual, 2 * size);
     const int64_t tiles = ((int64_t)q.M + 31) / 32;
     // Few tiles: a workgroup to 32 rows and 64 columns, eight wavefronts along k.  Many: the columns in turn, shared by as many
     // workgroups as it takes to have two to a compute unit.
     const bool few = tiles * a.groups <= 512 || !w;
-    a.splits = few ? a.groups : (int)std::max<int64_t>(1, std::min<int64_t>((a.groups + 3) / 4, 512 / tiles));
-    // 4 KiB of codes and 256 bytes of scales to 256 values of k; KW = 8 adds up in 64 KiB
-    constexpr size_t per_quad = 4096 + 256;
+    a.splits = few ? a.groups : (int)std::max<int64_t>(1, std::min<int64_t>((a.groups + 3) / 4, 1024 / tiles));
+    // besides, KW = 1 stores through 18 KiB, KW = 8 adds up in 64 KiB where the codes were
     a.chunk = (int)std::min<size_t>(a.quads, 139264 / per_quad);
     a.blocks = tdc_make_div(a.chunk * QUAD_BLOCKS);
-    const size_t lds = std::max<size_t>(a.chunk * per_quad, few ? 65536 : 0);
+    const size_t lds = few ? std::max<size_t>(a.chunk * per_quad, 65536) : a.chunk * per_quad + 4 * 16 * PITCH * sizeof(float);
     const unsigned wgs = (unsigned)(tiles * a.splits);
     const bool vectors = src.x && src.cols % 8 == 0 && tdc_aligned_to(src.x, 16) && src.pitch * size % 16 == 0;
     hipError_t e = hipErrorInvalidValue;

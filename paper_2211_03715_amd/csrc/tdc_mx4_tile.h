@@ -31,13 +31,18 @@ template <int OP> __device__ __forceinline__ tdc_f16v tdc_mx4_mfma(tdc_i4 a, uns
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(tdc_mx4_widen(a), tdc_mx4_widen(b), c, 4, 4, OP, (int)sa, OP, (int)sb);
 }
 
-// V sums of row m, from column n on, into y, which has rows of whole V's where V > 1.
+// V sums of row m, from column n on, into y, which has rows of whole V's and is read and written by V's where V > 1.
 template <typename T, int V> __device__ __forceinline__ void tdc_mx4_finish(const TdcMx4Product &q, float (&v)[V], int m, int n)
 {
     const size_t at = (size_t)m * q.N + n;
     if (q.epi.bias) {
+        constexpr int W = V < 4 ? V : 4;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += q.epi.bias[n + i];
+        for (int i = 0; i < V; i += W) {
+            const TdcVec<float, W> b = tdc_load<float, W>(q.epi.bias + n + i);
+#pragma unroll
+            for (int u = 0; u < W; ++u) v[i + u] += b.v[u];
+        }
     }
     if (q.epi.residual) {
         const TdcVec<T, V> r = tdc_load<T, V>(static_cast<const T *>(q.epi.residual) + at);
