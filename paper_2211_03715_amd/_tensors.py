@@ -4,9 +4,14 @@ from __future__ import annotations
 from . import binding as B
 
 
+_codes = {}
+
+
 def dtype_code(dtype) -> int:
-    import torch
-    code = {torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16}.get(dtype)
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16})
+    code = _codes.get(dtype)
     if code is None:
         raise ValueError("dtype must be torch.float32, float16 or bfloat16, not %s" % (dtype,))
     return code
@@ -18,10 +23,14 @@ def act_code(act: str) -> int:
     return B.ACTS[act]
 
 
+def _refuse(t, name, shape, dtype, device):
+    raise ValueError("%s must be %s %s on %s, not %s %s on %s" % (name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
+
+
 def expect(t, name: str, shape, dtype, device):
     """t is a contiguous tensor of that shape, dtype and device; returns it."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s %s on %s, not %s %s on %s" % (name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _refuse(t, name, shape, dtype, device)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return t
@@ -29,8 +38,8 @@ def expect(t, name: str, shape, dtype, device):
 
 def pixel_pitch(t, name: str, shape, dtype, device) -> int:
     """Elements from one pixel to the next of t [B][H][W][C], which may be a slice of the channels of wider pixels."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s %s on %s, not %s %s on %s" % (name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _refuse(t, name, shape, dtype, device)
     if t.is_contiguous():
         return shape[-1]
     b, h, w, c = shape
@@ -45,7 +54,7 @@ def stream_handle(stream, device) -> int:
     """The raw handle of a stream; None is the current stream of the TENSORS' device, whichever device is current."""
     if stream is None:
         import torch
-        return torch.cuda.current_stream(device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(device.index)   # what current_stream(device).cuda_stream is, without the objects
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -125,10 +125,22 @@ struct tdc_mx4_plan {
     TdcMx4Rows map;          // output pixel -> input pixel
     uint8_t *w_codes, *w_scales, *x_codes, *x_scales;   // plain: for large products, and what the others are laid out from
     uint8_t *w_laid, *ws_laid;                          // as tdc_mx4_rows.hip takes them
-    bool large;                                         // runs as a large product
+    bool large, first;                                  // runs as a large product; quantises x in a launch of its own
     bool packed;
     size_t ws_bytes;
 };
+
+namespace {
+
+// Rows in 4 bits times the plan's weights.
+int multiply(const tdc_mx4_plan *p, hipStream_t s, const uint8_t *codes, const uint8_t *scales, const TdcMx4Rows &rows, void *y, const tdc_mx4_epilogue *epilogue)
+{
+    const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, p->shape.N, tdc_mx4_blocks(p->shape.C), rows, y, kernel_epilogue(epilogue), false};
+    const hipError_t e = p->large ? tdc_launch_mx4_product(q, p->shape.dtype, s) : tdc_launch_mx4_rows(q, TdcMx4Source{nullptr, 0, 0}, p->shape.dtype, p->w_laid, p->ws_laid, s);
+    return e == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -203,7 +215,8 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     const size_t nb = tdc_mx4_blocks(s.C);
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     p->large = tdc_mx4_large(rows, s.N, s.C);
-    const size_t parts[6] = {up(s.N * nb * 16), up(s.N * nb), p->large ? up(rows * nb * 16) : 0, p->large ? up(rows * nb) : 0,
+    p->first = p->large || tdc_mx4_quantise_first(rows, s.N, s.C, tdc_dtype_bytes(s.dtype));
+    const size_t parts[6] = {up(s.N * nb * 16), up(s.N * nb), p->first ? up(rows * nb * 16) : 0, p->first ? up(rows * nb) : 0,
                              p->large ? 0 : tdc_mx4_laid_out_bytes(s.N, (int)nb), p->large ? 0 : tdc_mx4_laid_out_scale_bytes(s.N, (int)nb)};
     for (size_t n : parts) p->ws_bytes += n;
     if (hipMalloc((void **)&p->w_codes, p->ws_bytes) != hipSuccess) {
@@ -243,7 +256,7 @@ int tdc_mx4_plan_destroy(tdc_mx4_plan *p)
 
 size_t tdc_mx4_plan_workspace_bytes(const tdc_mx4_plan *p) { return p ? p->ws_bytes : 0; }
 
-int tdc_mx4_plan_kernel_count(const tdc_mx4_plan *p) { return !p ? 0 : p->large ? 2 : 1; }
+int tdc_mx4_plan_kernel_count(const tdc_mx4_plan *p) { return !p ? 0 : p->first ? 2 : 1; }
 
 int tdc_mx4_plan_pack(tdc_mx4_plan *p, void *hip_stream, const float *W)
 {
@@ -270,13 +283,12 @@ int tdc_conv_mx4(tdc_mx4_plan *p, void *hip_stream, const void *x, void *y, cons
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (!p->large) {
+    if (!p->first) {
         const TdcMx4Product q{nullptr, nullptr, nullptr, nullptr, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue), false};
         return tdc_launch_mx4_rows(q, TdcMx4Source{x, s.x_pitch, s.C}, s.dtype, p->w_laid, p->ws_laid, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
     }
     if (launch_quantize(st, x, s.dtype, p->map, p->rows, s.C, s.x_pitch, p->x_codes, p->x_scales) != hipSuccess) return TDC_ERR_HIP;
-    const TdcMx4Product q{p->x_codes, p->x_scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
-    return tdc_launch_mx4_product(q, s.dtype, st) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    return multiply(p, st, p->x_codes, p->x_scales, TdcMx4Rows::all(), y, epilogue);
 }
 
 int tdc_conv_mx4_quantized(tdc_mx4_plan *p, void *hip_stream, const uint8_t *codes, const uint8_t *scales, void *y, const tdc_mx4_epilogue *epilogue)
@@ -288,9 +300,7 @@ int tdc_conv_mx4_quantized(tdc_mx4_plan *p, void *hip_stream, const uint8_t *cod
     if (!tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(s.dtype))) return TDC_ERR_UNSUPPORTED;
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
-    const TdcMx4Product q{codes, scales, p->w_codes, p->w_scales, (int)p->rows, s.N, tdc_mx4_blocks(s.C), p->map, y, kernel_epilogue(epilogue), false};
-    if (!p->large) return tdc_launch_mx4_rows(q, TdcMx4Source{nullptr, 0, 0}, s.dtype, p->w_laid, p->ws_laid, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
-    return tdc_launch_mx4_product(q, s.dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    return multiply(p, (hipStream_t)hip_stream, codes, scales, p->map, y, epilogue);
 }
 
 }  // extern "C"

@@ -67,4 +67,12 @@ constexpr int TDC_MX4_MAX_COLS = 1 << 30;
 // A convolution that the matrix cores bound rather than memory runs as quantisation and a product in large tiles.
 inline bool tdc_mx4_large(int64_t rows, int N, int K) { return rows >= 4096 && N >= 1024 && K >= 1024; }
 
+// Whether tdc_launch_mx4_rows gives a workgroup 32 rows and only 64 columns, eight wavefronts along k.
+inline bool tdc_mx4_few(int64_t rows, int N) { return (rows + 31) / 32 * ((N + 63) / 64) <= 512; }
+
+// Every one of those quantises its rows of x anew, which takes longer than a launch where they have over 192 KB: 64 rows,
+// 4096 -> 4096 in bf16 (262 KB) 18.5 us, with x quantised in a launch of its own 10.3; 1568 rows, 2048 -> 512 in fp32 (262 KB)
+// 21.3 and 15.1; 6272 rows, 512 -> 128 in fp32 (66 KB) 7.8 and 11.0.
+inline bool tdc_mx4_quantise_first(int64_t rows, int N, int K, int size) { return tdc_mx4_few(rows, N) && (double)(rows < 32 ? rows : 32) * K * size > 192e3; }
+
 #endif  // TDC_MX4_INTERNAL_H

@@ -332,7 +332,7 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
     const int64_t tiles = ((int64_t)q.M + 31) / 32;
     // Few tiles: a workgroup to 32 rows and 64 columns, eight wavefronts along k.  Many: the columns in turn, shared by as many
     // workgroups as it takes to have two to a compute unit.
-    const bool few = tiles * a.groups <= 512 || !w;
+    const bool few = tdc_mx4_few(q.M, q.N) || !w;
     a.splits = few ? a.groups : (int)std::max<int64_t>(1, std::min<int64_t>((a.groups + 3) / 4, 1024 / tiles));
     // besides, KW = 1 stores through 18 KiB, KW = 8 adds up in 64 KiB where the codes were
     a.chunk = (int)std::min<size_t>(a.quads, 139264 / per_quad);

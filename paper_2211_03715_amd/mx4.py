@@ -13,20 +13,16 @@ from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stre
 from .layer import _order_after, _torch_stream
 
 
-class _current:
-    """Calls without a plan run on the current device: make it the tensors'."""
-
-    def __init__(self, device):
-        import torch
-        self.context = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.context is not None:
-            self.context.__enter__()
-
-    def __exit__(self, *exc):
-        if self.context is not None:
-            self.context.__exit__(*exc)
+def _call(fn, device, stream, *args, name):
+    """A call without a plan runs on the current device: make it the tensors'."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        rc = fn(stream_handle(stream, device), *args)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(stream_handle(stream, device), *args)
+    if rc:
+        raise B.TdcError(rc, name)
 
 
 def _row_pitch(x):
@@ -65,21 +61,19 @@ def quantize(x, stream=None):
     code = dtype_code(x.dtype)
     if not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must be a tensor on a GPU with a last dimension of at least one value")
-    C, lead = x.shape[-1], tuple(x.shape[:-1])
-    nb, rows, pitch = -(-C // 32), _rows(lead), _row_pitch(x)
-    with _current(x.device), on_stream(stream, x.device, (x,)):
-        codes = torch.empty(lead + (nb * 16,), device=x.device, dtype=torch.uint8)
-        scales = torch.empty(lead + (nb,), device=x.device, dtype=torch.uint8)
-        rc = B.load().tdc_mx4_quantize(stream_handle(stream, x.device), x.data_ptr(), code, rows, C, pitch, codes.data_ptr(), scales.data_ptr())
-    if rc:
-        raise B.TdcError(rc, "tdc_mx4_quantize")
+    C, lead, device = x.shape[-1], x.shape[:-1], x.device
+    nb, pitch = -(-C // 32), _row_pitch(x)
+    with on_stream(stream, device, (x,)):
+        codes = torch.empty(lead + (nb * 16,), device=device, dtype=torch.uint8)
+        scales = torch.empty(lead + (nb,), device=device, dtype=torch.uint8)
+    _call(B.load().tdc_mx4_quantize, device, stream, x.data_ptr(), code, x.numel() // C, C, pitch, codes.data_ptr(), scales.data_ptr(), name="tdc_mx4_quantize")
     return codes, scales
 
 
 def _pair(codes, scales, C, name):
     """Checks a quantised tensor of rows of C values; returns its leading dimensions."""
     import torch
-    nb, lead = -(-C // 32), tuple(codes.shape[:-1])
+    nb, lead = -(-C // 32), codes.shape[:-1]
     if not codes.is_cuda:
         raise ValueError("%s must be on a GPU" % name)
     expect(codes, name + " codes", lead + (nb * 16,), torch.uint8, codes.device)
@@ -93,12 +87,10 @@ def dequantize(codes, scales, C: int, dtype=None, stream=None):
     if C < 1:
         raise ValueError("C must be at least 1")
     dtype = dtype or torch.float32
-    lead, code = _pair(codes, scales, C, "x"), dtype_code(dtype)
-    with _current(codes.device), on_stream(stream, codes.device, (codes, scales)):
-        y = torch.empty(lead + (C,), device=codes.device, dtype=dtype)
-        rc = B.load().tdc_mx4_dequantize(stream_handle(stream, codes.device), codes.data_ptr(), scales.data_ptr(), _rows(lead), C, y.data_ptr(), code, 0)
-    if rc:
-        raise B.TdcError(rc, "tdc_mx4_dequantize")
+    lead, code, device = _pair(codes, scales, C, "x"), dtype_code(dtype), codes.device
+    with on_stream(stream, device, (codes, scales)):
+        y = torch.empty(lead + (C,), device=device, dtype=dtype)
+    _call(B.load().tdc_mx4_dequantize, device, stream, codes.data_ptr(), scales.data_ptr(), _rows(lead), C, y.data_ptr(), code, 0, name="tdc_mx4_dequantize")
     return y
 
 
@@ -115,12 +107,10 @@ def matmul(a, b, K: int, bias=None, residual=None, act: str = "none", dtype=None
     bias_p = None if bias is None else expect(bias, "bias", (N,), torch.float32, dev).data_ptr()
     res_p = None if residual is None else expect(residual, "residual", lead + (N,), dtype, dev).data_ptr()
     epi = B.tdc_mx4_epilogue(bias_p, res_p, act_code(act))
-    with _current(dev), on_stream(stream, dev, a + b + (bias, residual)):
+    with on_stream(stream, dev, tuple(a) + tuple(b) + (bias, residual)):
         y = torch.empty(lead + (N,), device=dev, dtype=dtype) if y is None else expect(y, "y", lead + (N,), dtype, dev)
-        rc = B.load().tdc_mx4_matmul(stream_handle(stream, dev), a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(), _rows(lead), N, K,
-                                     y.data_ptr(), code, ctypes.byref(epi))
-    if rc:
-        raise B.TdcError(rc, "tdc_mx4_matmul")
+    _call(B.load().tdc_mx4_matmul, dev, stream, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(), _rows(lead), N, K, y.data_ptr(), code, ctypes.byref(epi),
+          name="tdc_mx4_matmul")
     return y
 
 
@@ -140,11 +130,12 @@ class MX4Conv2d:
         self.layer, self.dtype = layer, dtype or torch.float32
         self.dev = torch.device("cuda", device)
         self.x_pitch = x_pitch or layer.C
+        self._in, self._out = (layer.batch, layer.H, layer.W, layer.C), (layer.batch, (layer.H - 1) // layer.stride + 1, (layer.W - 1) // layer.stride + 1, layer.N)
+        self._pack_event = None
         self.plan = B.tdc_mx4_plan_create(B.tdc_mx4_shape(layer.batch, layer.H, layer.W, layer.C, layer.N, layer.stride, dtype_code(self.dtype), self.x_pitch), device)
 
     def out_shape(self):
-        L = self.layer
-        return (L.batch, (L.H - 1) // L.stride + 1, (L.W - 1) // L.stride + 1, L.N)
+        return self._out
 
     def kernel_count(self) -> int:
         return B.tdc_mx4_plan_kernel_count(self.plan)
@@ -164,10 +155,10 @@ class MX4Conv2d:
         self._pack_event = ts.record_event()
         self._ordered = {ts.cuda_stream}
 
-    def _call(self, x, y, bias, residual, act):
+    def _arguments(self, x, y, bias, residual, act):
         import torch
         L = self.layer
-        shape, out = (L.batch, L.H, L.W, L.C), self.out_shape()
+        shape, out = self._in, self._out
         if isinstance(x, (tuple, list)):
             if _rows(_pair(*x, L.C, "x")) != L.batch * L.H * L.W or x[0].device != self.dev:
                 raise ValueError("x must hold one row of %d values for each of %d pixels on %s" % (L.C, L.batch * L.H * L.W, self.dev))
@@ -179,19 +170,22 @@ class MX4Conv2d:
             fn, ins = B.load().tdc_conv_mx4, (x.data_ptr(),)
         bias_p = None if bias is None else expect(bias, "bias", (L.N,), torch.float32, self.dev).data_ptr()
         res_p = None if residual is None else expect(residual, "residual", out, self.dtype, self.dev).data_ptr()
-        epi = B.tdc_mx4_epilogue(bias_p, res_p, act_code(act))
-        return fn, ins + (expect(y, "y", out, self.dtype, self.dev).data_ptr(), ctypes.byref(epi))
+        code = act_code(act)
+        epi = ctypes.byref(B.tdc_mx4_epilogue(bias_p, res_p, code)) if bias_p or res_p or code else None
+        return fn, ins + (expect(y, "y", out, self.dtype, self.dev).data_ptr(), epi)
 
     def __call__(self, x, y=None, bias=None, residual=None, act: str = "none", stream=None):
         """y = act(conv(x) + bias[n] + residual)."""
         import torch
-        if getattr(self, "_pack_event", None) is not None:
+        if self._pack_event is not None:
             _order_after(self, stream if stream is not None else torch.cuda.current_stream(self.dev))
-        with on_stream(stream, self.dev, (tuple(x) if isinstance(x, (tuple, list)) else (x,)) + (bias, residual)):
-            if y is None:
-                y = torch.empty(self.out_shape(), device=self.dev, dtype=self.dtype)
-            fn, args = self._call(x, y, bias, residual, act)
-            rc = fn(self.plan, stream_handle(stream, self.dev), *args)
+        if stream is not None:
+            with on_stream(stream, self.dev, (tuple(x) if isinstance(x, (tuple, list)) else (x,)) + (bias, residual)):
+                y = torch.empty(self._out, device=self.dev, dtype=self.dtype) if y is None else y
+        elif y is None:
+            y = torch.empty(self._out, device=self.dev, dtype=self.dtype)
+        fn, args = self._arguments(x, y, bias, residual, act)
+        rc = fn(self.plan, stream_handle(stream, self.dev), *args)
         if rc:
             raise B.TdcError(rc, "tdc_conv_mx4")
         return y
@@ -199,9 +193,9 @@ class MX4Conv2d:
     def bind(self, x, y, bias=None, residual=None, act: str = "none", stream=None):
         """A zero-argument launcher with the arguments marshalled once.  The tensors and the stream must outlive it."""
         import torch
-        if getattr(self, "_pack_event", None) is not None:
+        if self._pack_event is not None:
             _order_after(self, stream if stream is not None else torch.cuda.current_stream(self.dev))
-        fn, args = self._call(x, y, bias, residual, act)
+        fn, args = self._arguments(x, y, bias, residual, act)
         plan, handle = self.plan, ctypes.c_void_p(stream_handle(stream, self.dev))
         args = tuple(ctypes.c_void_p(a) if isinstance(a, int) else a for a in args)
 

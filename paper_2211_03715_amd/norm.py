@@ -11,6 +11,11 @@ from . import binding as B
 from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stream_handle
 
 
+def _float32():
+    import torch
+    return torch.float32
+
+
 class GroupNorm:
     """y = act(group_norm(x) * gamma + beta + residual) on x [batch][H][W][C] with C/groups neighbouring channels to a group.
 
@@ -22,6 +27,7 @@ class GroupNorm:
         self.plan = None
         self.dtype = dtype or torch.float32
         self.shape = (batch, H, W, C)
+        self._blocks = -(-C // 32)
         self.groups = groups
         self.act = act_code(act)
         self.dev = torch.device("cuda", device)
@@ -38,26 +44,24 @@ class GroupNorm:
     def new_quantized(self):
         """(codes, scales) for quantized(): rows of C values in 4 bits, see mx4.py."""
         import torch
-        nb = -(-self.shape[3] // 32)
-        return (torch.empty(self.shape[:3] + (nb * 16,), device=self.dev, dtype=torch.uint8), torch.empty(self.shape[:3] + (nb,), device=self.dev, dtype=torch.uint8))
+        return tuple(torch.empty(self.shape[:3] + (self._blocks * n,), device=self.dev, dtype=torch.uint8) for n in (16, 1))
 
     def _channel(self, t, name):
-        import torch
-        return None if t is None else expect(t, name, self.shape[3:], torch.float32, self.dev).data_ptr()
+        return None if t is None else expect(t, name, self.shape[3:], _float32(), self.dev).data_ptr()
 
     def _pixels(self, t, name):
         return (None, 0) if t is None else (t.data_ptr(), pixel_pitch(t, name, self.shape, self.dtype, self.dev))
 
     def _stats(self, stats):
-        import torch
         if stats is None:
             return None, None
         mean, rstd = stats
-        return tuple(expect(t, n, (self.shape[0], self.groups), torch.float32, self.dev).data_ptr() for t, n in ((mean, "mean"), (rstd, "rstd")))
+        return tuple(expect(t, n, (self.shape[0], self.groups), _float32(), self.dev).data_ptr() for t, n in ((mean, "mean"), (rstd, "rstd")))
 
     def _forward(self, x, gamma, beta, residual, stats, y=None, quantized=None):
         """The foreign function of a forward call and its arguments behind the stream, and what they refer to."""
         import torch
+        C = self.shape[3]
         xp, x_pitch = self._pixels(x, "x")
         rp, r_pitch = self._pixels(residual, "residual")
         mean, rstd = self._stats(stats)
@@ -66,21 +70,25 @@ class GroupNorm:
             fn, out = B.load().tdc_group_norm, (yp,)
         else:
             codes, scales = quantized
-            nb, y_pitch = -(-self.shape[3] // 32), 0
+            y_pitch = C
             fn = B.load().tdc_group_norm_mx4
-            out = (expect(codes, "codes", self.shape[:3] + (nb * 16,), torch.uint8, self.dev).data_ptr(),
-                   expect(scales, "scales", self.shape[:3] + (nb,), torch.uint8, self.dev).data_ptr())
-        args = B.tdc_norm_args(rp, mean, rstd, x_pitch, r_pitch, y_pitch)
-        return fn, (xp, self._channel(gamma, "gamma"), self._channel(beta, "beta")) + out + (ctypes.byref(args),)
+            out = (expect(codes, "codes", self.shape[:3] + (self._blocks * 16,), torch.uint8, self.dev).data_ptr(),
+                   expect(scales, "scales", self.shape[:3] + (self._blocks,), torch.uint8, self.dev).data_ptr())
+        args = None
+        if rp or mean or x_pitch != C or y_pitch != C:
+            args = ctypes.byref(B.tdc_norm_args(rp, mean, rstd, x_pitch, r_pitch, y_pitch))
+        return fn, (xp, self._channel(gamma, "gamma"), self._channel(beta, "beta")) + out + (args,)
 
     def __call__(self, x, gamma=None, beta=None, residual=None, y=None, stats=None, stream=None):
         """Returns y (a new contiguous tensor unless given).  ``stats``: new_stats(), filled for backward()."""
         import torch
-        with on_stream(stream, self.dev, (x, gamma, beta, residual)):
-            if y is None:
-                y = torch.empty(self.shape, device=self.dev, dtype=self.dtype)
-            fn, args = self._forward(x, gamma, beta, residual, stats, y)
-            rc = fn(self.plan, stream_handle(stream, self.dev), *args)
+        if stream is not None:
+            with on_stream(stream, self.dev, (x, gamma, beta, residual)):
+                y = torch.empty(self.shape, device=self.dev, dtype=self.dtype) if y is None else y
+        elif y is None:
+            y = torch.empty(self.shape, device=self.dev, dtype=self.dtype)
+        fn, args = self._forward(x, gamma, beta, residual, stats, y)
+        rc = fn(self.plan, stream_handle(stream, self.dev), *args)
         if rc:
             raise B.TdcError(rc, "tdc_group_norm")
         return y
@@ -117,20 +125,23 @@ class GroupNorm:
         """(dx, dgamma, dbeta, dresidual) from the statistics that the forward call filled.  gamma, beta and residual are the
         forward call's; dresidual is None without a residual."""
         import torch
+        C = self.shape[3]
         mean, rstd = self._stats(stats)
         with on_stream(stream, self.dev, (x, dy, gamma, beta, residual) + tuple(stats)):
             dx = torch.empty(self.shape, device=self.dev, dtype=self.dtype)
-            grads = torch.empty((2, self.shape[3]), device=self.dev, dtype=torch.float32)
-            dres = None if residual is None else torch.empty_like(dx)
-            xp, x_pitch = self._pixels(x, "x")
-            dyp, dy_pitch = self._pixels(dy, "dy")
-            rp, r_pitch = self._pixels(residual, "residual")
-            args = B.tdc_norm_grad_args(rp, None if dres is None else dres.data_ptr(), x_pitch, r_pitch, dy_pitch, 0, 0)
-            rc = B.load().tdc_group_norm_backward(self.plan, stream_handle(stream, self.dev), xp, dyp, mean, rstd, self._channel(gamma, "gamma"),
-                                                  self._channel(beta, "beta"), dx.data_ptr(), grads.data_ptr(), grads.data_ptr() + 4 * self.shape[3], ctypes.byref(args))
+            dgamma, dbeta = torch.empty((2, C), device=self.dev, dtype=torch.float32).unbind(0)
+            dres = None if residual is None else torch.empty(self.shape, device=self.dev, dtype=self.dtype)
+        xp, x_pitch = self._pixels(x, "x")
+        dyp, dy_pitch = self._pixels(dy, "dy")
+        rp, r_pitch = self._pixels(residual, "residual")
+        args = None
+        if rp or x_pitch != C or dy_pitch != C:
+            args = ctypes.byref(B.tdc_norm_grad_args(rp, None if dres is None else dres.data_ptr(), x_pitch, r_pitch, dy_pitch, 0, 0))
+        rc = B.load().tdc_group_norm_backward(self.plan, stream_handle(stream, self.dev), xp, dyp, mean, rstd, self._channel(gamma, "gamma"),
+                                              self._channel(beta, "beta"), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), args)
         if rc:
             raise B.TdcError(rc, "tdc_group_norm_backward")
-        return dx, grads[0], grads[1], dres
+        return dx, dgamma, dbeta, dres
 
     def close(self) -> None:
         if self.plan is not None:
