@@ -6,32 +6,44 @@
 
 namespace {
 
-// ---- x -> codes and scales: a thread to a block
-template <typename T, int V>
-__global__ __launch_bounds__(256) void tdc_mx4_quantize_blocks(const T *__restrict__ x, TdcMx4Rows rows, int64_t total, int cols, int nb, int64_t pitch,
-                                                               uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
+// ---- x -> codes and scales: V neighbours to a lane, 16 bytes of x, or one by one where rows do not come in such pieces;
+// 32 / V neighbouring lanes to a block.  Four pieces to a thread, 256 threads apart: what a wavefront reads, and writes, at a time
+// is whole lines.
+template <typename T, int V, bool VECTORS>
+__global__ __launch_bounds__(256) void tdc_mx4_quantize_lanes(const T *__restrict__ x, TdcMx4Rows rows, int64_t total, int cols, TdcMx4Div blocks, int64_t pitch,
+                                                              uint8_t *__restrict__ codes, uint8_t *__restrict__ scales)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int64_t m = i / nb;
-    const int kb = (int)(i - m * nb), c0 = kb * 32;
-    const T *p = x + rows.source(m) * pitch + c0;
-    float v[32];
+    constexpr int U = 4, LANES = 32 / V;
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t first = (int64_t)blockIdx.x * (256 * U / LANES) + threadIdx.x / LANES;
+    float v[U][V];
 #pragma unroll
-    for (int j = 0; j < 32; j += V) {
-        if (c0 + j < cols) {
-            const TdcVec<T, V> in = tdc_load<T, V>(p + j);
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = min(first + u * (256 / LANES), total - 1), m = blocks.of(i);
+        const int c0 = (int)(i - m * blocks.d) * 32 + lane * V;
+        const T *p = x + rows.source(m) * pitch + c0;
+        if constexpr (VECTORS) {
+            TdcVec<T, V> in;
+            if (c0 < cols) in = tdc_load<T, V>(p);             // V divides cols: all of them or none
 #pragma unroll
-            for (int u = 0; u < V; ++u) v[j + u] = (float)in.v[u];
+            for (int j = 0; j < V; ++j) v[u][j] = c0 < cols ? (float)in.v[j] : 0.f;
         } else {
 #pragma unroll
-            for (int u = 0; u < V; ++u) v[j + u] = 0.f;
+            for (int j = 0; j < V; ++j) v[u][j] = c0 + j < cols ? (float)p[j] : 0.f;
         }
     }
-    unsigned e;
-    const tdc_i4 c = tdc_mx4_block(v, e);
-    *reinterpret_cast<tdc_i4 *>(codes + i * 16) = c;
-    scales[i] = (uint8_t)e;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) top = max(top, tdc_abs_bits(v[u][j]));
+        const unsigned e = tdc_mx4_scale(tdc_lane_max<LANES>(top));
+        const int64_t i = first + u * (256 / LANES);
+        if (i >= total) break;
+        if constexpr (V == 8) reinterpret_cast<unsigned *>(codes)[i * LANES + lane] = tdc_mx4_codes8(v[u], e);
+        else reinterpret_cast<uint16_t *>(codes)[i * LANES + lane] = (uint16_t)tdc_mx4_codes4(v[u], e);
+        if (lane == 0) scales[i] = (uint8_t)e;
+    }
 }
 
 // ---- W[C][N] -> codes and scales of [N][C]: a thread to a block, neighbours along N
@@ -50,38 +62,44 @@ __global__ __launch_bounds__(256) void tdc_mx4_pack_weights(const float *__restr
     }
 }
 
-// ---- codes and scales -> values, a thread to eight of them
-template <typename T, int V>
-__global__ __launch_bounds__(256) void tdc_mx4_dequantize_values(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t total, int cols, int nb,
-                                                                 int64_t pitch, T *__restrict__ y)
+// ---- codes and scales -> values, laid over the lanes the same way
+template <typename T, int V, bool VECTORS>
+__global__ __launch_bounds__(256) void tdc_mx4_dequantize_lanes(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t total, int cols, TdcMx4Div blocks,
+                                                                int64_t pitch, T *__restrict__ y)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int64_t block = i >> 2, m = block / nb;
-    const int c0 = (int)(block - m * nb) * 32 + (int)(i & 3) * 8;
-    if (c0 >= cols) return;
-    const unsigned c = reinterpret_cast<const unsigned *>(codes)[i];
-    float v[8];
-    tdc_mx4_values8(c, scales[block], v);
-    T *out = y + m * pitch + c0;
+    constexpr int U = 4, LANES = 32 / V;
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t first = (int64_t)blockIdx.x * (256 * U / LANES) + threadIdx.x / LANES;
+    unsigned c[U], e[U];
 #pragma unroll
-    for (int j = 0; j < 8; j += V) {
-        if (c0 + j < cols) {
-            float o[V];
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = min(first + u * (256 / LANES), total - 1);
+        c[u] = V == 8 ? reinterpret_cast<const unsigned *>(codes)[i * LANES + lane] : reinterpret_cast<const uint16_t *>(codes)[i * LANES + lane];
+        e[u] = scales[i];
+    }
 #pragma unroll
-            for (int u = 0; u < V; ++u) o[u] = v[j + u];
-            tdc_store<T, V>(out + j, o);
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = first + u * (256 / LANES), m = blocks.of(i);
+        const int c0 = (int)(i - m * blocks.d) * 32 + lane * V;
+        if (i >= total) break;
+        float v[V];
+        tdc_mx4_values(c[u], e[u], v);
+        T *out = y + m * pitch + c0;
+        if constexpr (VECTORS) {
+            if (c0 < cols) tdc_store<T, V>(out, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (c0 + j < cols) out[j] = (T)v[j];
         }
     }
 }
 
-// The most neighbours that one access of rows of `cols` may take.
-int row_vec(int dtype, int64_t cols, int64_t pitch, const void *p)
+// Whether rows come in pieces of 16 bytes.
+bool row_vectors(int dtype, int64_t cols, int64_t pitch, const void *p)
 {
-    const int size = tdc_dtype_bytes(dtype);
-    for (int v = 16 / size; v > 1; v /= 2)
-        if (cols % v == 0 && pitch % v == 0 && tdc_aligned_to(p, (size_t)v * size)) return v;
-    return 1;
+    const int v = 16 / tdc_dtype_bytes(dtype);
+    return cols % v == 0 && pitch % v == 0 && tdc_aligned_to(p, 16);
 }
 
 // Workgroups of a launch along x; 0 where there are too many.
@@ -95,11 +113,14 @@ hipError_t launch_quantize(hipStream_t s, const void *x, int dtype, const TdcMx4
 {
     const int nb = tdc_mx4_blocks(cols);
     const int64_t total = n_rows * nb;
-    const unsigned grid = blocks_for(total, 256);
-    if (!grid) return hipErrorInvalidValue;
-    TDC_FOR_DTYPE(dtype, T, TDC_FOR_VEC(row_vec(dtype, cols, pitch, x), T, V, {
-        tdc_mx4_quantize_blocks<T, V><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, nb, pitch, codes, scales);
-    }));
+    const bool vectors = row_vectors(dtype, cols, pitch, x);
+    TDC_FOR_DTYPE(dtype, T, {
+        constexpr int V = 16 / sizeof(T);
+        const unsigned grid = blocks_for(total, 32 * V);   // 1024 pieces of V
+        if (!grid) return hipErrorInvalidValue;
+        if (vectors) tdc_mx4_quantize_lanes<T, V, true><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, TdcMx4Div(nb), pitch, codes, scales);
+        else tdc_mx4_quantize_lanes<T, V, false><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, TdcMx4Div(nb), pitch, codes, scales);
+    });
     return hipGetLastError();
 }
 
@@ -151,7 +172,7 @@ int tdc_mx4_quantize(void *hip_stream, const void *x, int dtype, int64_t rows, i
     if (pitch == 0) pitch = cols;
     if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
     if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(x, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
-    if (rows > INT64_MAX / 64 / tdc_mx4_blocks((int)cols) || !blocks_for(rows * tdc_mx4_blocks((int)cols), 256)) return TDC_ERR_UNSUPPORTED;
+    if (rows > INT64_MAX / 64 / tdc_mx4_blocks((int)cols) || !blocks_for(rows * tdc_mx4_blocks((int)cols), 128)) return TDC_ERR_UNSUPPORTED;
     return launch_quantize((hipStream_t)hip_stream, x, dtype, TdcMx4Rows::all(), rows, (int)cols, pitch, codes, scales) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
@@ -164,13 +185,16 @@ int tdc_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint8_t *sc
     if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     const int nb = tdc_mx4_blocks((int)cols);
     if (rows > INT64_MAX / 64 / nb) return TDC_ERR_UNSUPPORTED;
-    const int64_t total = rows * nb * 4;
-    const unsigned grid = blocks_for(total, 256);
-    if (!grid) return TDC_ERR_UNSUPPORTED;
+    const int64_t total = rows * nb;
+    if (!blocks_for(total, 128)) return TDC_ERR_UNSUPPORTED;
     hipStream_t s = (hipStream_t)hip_stream;
-    TDC_FOR_DTYPE(dtype, T, TDC_FOR_VEC(row_vec(dtype, cols, pitch, y), T, V, {
-        tdc_mx4_dequantize_values<T, V><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, nb, pitch, (T *)y);
-    }));
+    const bool vectors = row_vectors(dtype, cols, pitch, y);
+    TDC_FOR_DTYPE(dtype, T, {
+        constexpr int V = 16 / sizeof(T);
+        const unsigned grid = blocks_for(total, 32 * V);
+        if (vectors) tdc_mx4_dequantize_lanes<T, V, true><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, TdcMx4Div(nb), pitch, (T *)y);
+        else tdc_mx4_dequantize_lanes<T, V, false><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, TdcMx4Div(nb), pitch, (T *)y);
+    });
     return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
@@ -201,7 +225,7 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS) return TDC_ERR_UNSUPPORTED;
     if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
     const int64_t rows = s.batch * Ho * Wo;
-    if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 256)) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 128)) return TDC_ERR_UNSUPPORTED;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev) return TDC_ERR_HIP;
     DeviceGuard guard(device);

@@ -55,14 +55,14 @@ __device__ __forceinline__ tdc_i4 tdc_mx4_block(const float (&v)[32], unsigned &
     return (tdc_i4){(int)tdc_mx4_codes8(v, e), (int)tdc_mx4_codes8(v + 8, e), (int)tdc_mx4_codes8(v + 16, e), (int)tdc_mx4_codes8(v + 24, e)};
 }
 
-// Eight codes as values.  e = 255: all NaN.
-__device__ __forceinline__ void tdc_mx4_values8(unsigned c, unsigned e, float (&v)[8])
+// V codes as values.  e = 255: all NaN.
+template <int V> __device__ __forceinline__ void tdc_mx4_values(unsigned c, unsigned e, float (&v)[V])
 {
     // 2^(e - 127) in two factors, so that e = 0 and values below the normal range come out exactly
     const int up = (int)e - 127, half = up / 2;
     const float s1 = __builtin_bit_cast(float, (unsigned)(127 + half) << 23), s2 = __builtin_bit_cast(float, (unsigned)(127 + up - half) << 23);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < V; ++i) {
         const unsigned m = (c >> (4 * i)) & 7u, sign = (c >> (4 * i + 3)) & 1u;
         // magnitude code m: 0, 1/2, then (1 + (m & 1)/2) 2^((m >> 1) - 1)
         const float mag = m < 2u ? 0.5f * m : __builtin_bit_cast(float, ((126u + (m >> 1)) << 23) | ((m & 1u) << 22));

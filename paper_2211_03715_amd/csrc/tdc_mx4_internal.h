@@ -2,6 +2,7 @@
 #ifndef TDC_MX4_INTERNAL_H
 #define TDC_MX4_INTERNAL_H
 
+#include "tdc_div.h"
 #include "tdc_mx4_device.h"
 #include "tdc_typed.h"
 
@@ -18,6 +19,19 @@ struct TdcMx4Rows {
         const int64_t b = m / HoWo;
         const int q = (int)(m - b * HoWo), i = q / Wo, j = q - i * Wo;
         return b * HW + (int64_t)i * stride * W + (int64_t)j * stride;
+    }
+};
+
+// Division of 64-bit indices by a launch-time constant: by 32-bit multiplication where the index allows it.
+struct TdcMx4Div {
+    int d;
+    TdcDiv by;
+    explicit TdcMx4Div(int n) : d(n), by(tdc_make_div(n)) {}
+    __device__ int64_t of(int64_t i) const
+    {
+        if (i >> 32) return i / d;
+        const unsigned u = (unsigned)i;
+        return tdc_div_from_hi(u, __umulhi(by.m, u), by);
     }
 };
 

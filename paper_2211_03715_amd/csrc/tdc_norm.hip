@@ -100,20 +100,32 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
     Affine<V> a;
     a.set(d, in, stats, c0 / d.Cg, c0 + (live ? t.cv * V : 0));
     const T *res = in.residual ? static_cast<const T *>(in.residual) + (size_t)b * d.P * in.rp + c0 + t.cv * V : nullptr;
-    // MX4: lanes that share a block have the same pixels, but their neighbours in the wavefront may have one less
+    // MX4: lanes that share a block have the same pixels, but their neighbours in the wavefront may have one less.  The residual
+    // comes four pixels at a time: behind a store, which might change it for all the compiler knows, each would wait by itself.
+    constexpr int R = HELD < 4 ? HELD : 4;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const int p = tdc_anew(t.r + i * t.rows);
-        const bool mine = live && p < d.P;
-        if (MX4 ? i >= held_here : !mine) break;
-        tdc_forget(held[i]);
-        TdcVec<T, V> rv;
-        if (res && mine) rv = tdc_load<T, V>(res + (size_t)p * in.rp);
-        float o[V];
-        apply(a, held[i], rv, in, o);
-        const size_t px = (size_t)b * d.P + p;
-        if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
-        else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
+    for (int i0 = 0; i0 < HELD; i0 += R) {
+        if (i0 >= held_here) break;
+        TdcVec<T, V> rv[R];
+        if (res) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int p = tdc_anew(t.r + (i0 + i) * t.rows);
+                if (live && p < d.P) rv[i] = tdc_load<T, V>(res + (size_t)p * in.rp);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int p = tdc_anew(t.r + (i0 + i) * t.rows);
+            const bool mine = live && p < d.P;
+            if (MX4 ? i0 + i >= held_here : !mine) break;
+            tdc_forget(held[i0 + i]);
+            float o[V];
+            apply(a, held[i0 + i], rv[i], in, o);
+            const size_t px = (size_t)b * d.P + p;
+            if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
+            else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
+        }
     }
 }
 
