@@ -45,15 +45,15 @@ typedef struct tdc_mx4_epilogue {
 } tdc_mx4_epilogue;
 
 /* y[M][N] = A[M][K] B[N][K]^T: both operands in rows of K values in 4 bits; y is stored in `dtype`.
- * M = 0 is accepted and does nothing. */
+ * M = 0 is accepted and does nothing.  TDC_ERR_UNSUPPORTED for N over 2^24. */
 int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                    const uint8_t *b_scales, int32_t M, int32_t N, int32_t K, void *y, int dtype,
                    const tdc_mx4_epilogue *epilogue);
 
 /* A 1x1 convolution on channels-last images with weights in 4 bits: x [batch][H][W][C] -> y [batch][Ho][Wo][N], with
  * Ho = ceil(H/stride), Wo = ceil(W/stride); output (i, j) reads input (i*stride, j*stride).  x_pitch: elements from one input
- * pixel to the next (0: C; else at least C).  TDC_ERR_UNSUPPORTED for an unknown dtype or when batch*H*W, or batch*Ho*Wo*N / 32,
- * reaches 2^31. */
+ * pixel to the next (0: C; else at least C).  TDC_ERR_UNSUPPORTED for an unknown dtype, for N over 2^24, or when batch*H*W, or
+ * batch*Ho*Wo*N / 32, reaches 2^31. */
 typedef struct tdc_mx4_shape {
     int32_t batch, H, W, C, N, stride;
     int32_t dtype;                /* of x, y and residual */

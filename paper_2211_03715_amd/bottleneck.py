@@ -22,13 +22,24 @@ TuckerBasicBlock is the two-convolution block of the shallower networks, both 3x
 and TuckerResNet18Body the 2 + 2 + 2 + 2 of them of a ResNet-18-shaped network (16 Tucker layers: the shapes of the
 batch-1 benchmark sweep, in sequence, with their shortcuts and epilogues).
 
+TuckerNormBottleneck is the bottleneck block with group norm instead of a folded batch norm, for networks that are fine-tuned
+with small batches, and with its 1x1 weights in 4 bits (channels last):
+    t1 = W1 (*) x                              1x1, weights and x in 4 bits        tdc_conv_mx4
+    n1 = relu(norm(t1))                                                           tdc_group_norm
+    t2 = Tucker3x3(n1)                                                            tdc_conv_tucker2_ex
+    q2 = relu(norm(t2)), stored in 4 bits                                          tdc_group_norm_mx4
+    t3 = W3 (*) q2                             1x1, both in 4 bits                 tdc_conv_mx4_quantized
+    y  = relu(norm(t3) + s(x))                 s(x) = x, or norm(Wp (*) x)         tdc_group_norm
+
     python -m paper_2211_03715_amd.bottleneck [--nhwc]             # eager vs graph latency of a few block shapes
     python -m paper_2211_03715_amd.bottleneck --resnet50 [--nhwc] [--batch B]   # the 16-block network
     python -m paper_2211_03715_amd.bottleneck --resnet18 [--nhwc] [--batch B]   # the 8 basic blocks
+    python -m paper_2211_03715_amd.bottleneck --resnet50 --norm [--batch B]     # 16 blocks with group norm and 4-bit 1x1 weights
     ... --oracle    # then once more with every convolution's tuning found by exhaustive search (minutes)
 """
 from __future__ import annotations
 
+import math
 import sys
 from typing import Dict
 
@@ -145,6 +156,83 @@ class TuckerBottleneck:
             c.close()
 
 
+def make_norm_block_weights(C: int, M: int, R1: int, R2: int, seed: int, C_out: int = 0, projection: bool = False) -> Dict[str, np.ndarray]:
+    """make_block_weights' convolutions with a scale and a shift to each channel behind them ("g1", "b1" ..; "gp", "bp")."""
+    w = make_block_weights(C, M, R1, R2, seed, C_out, projection)
+    rng = np.random.default_rng(seed + 1)
+    for k in ("1", "2", "3") + (("p",) if projection else ()):
+        w["g" + k] = 1 + np.float32(0.2) * rng.standard_normal(w["b" + k].shape, dtype=np.float32)
+    return w
+
+
+class TuckerNormBottleneck(TuckerBottleneck):
+    def __init__(self, batch: int, C: int, M: int, H: int, W: int, R1: int, R2: int, weights: Dict, device: int = 0,
+                 layout: int = B.LAYOUT_NHWC, stride: int = 1, C_out: int = 0, tunings=None, groups: int = 32):
+        """A bottleneck with group norms of ``groups`` groups (fewer where they do not divide the channels: their greatest
+        common divisor) and 4-bit 1x1 convolutions, channels last.  ``weights``: make_norm_block_weights; ``tunings`` as in
+        TuckerBottleneck, for the Tucker layer."""
+        import torch
+        from .mx4 import MX4Conv2d
+        from .norm import GroupNorm
+        if layout != B.LAYOUT_NHWC:
+            raise ValueError("blocks with group norm are channels last")
+        self.dev = torch.device("cuda", device)
+        self.layout = layout
+        C_out = C_out or C
+        self.projection = stride != 1 or C_out != C
+        self.l1 = Layer(batch, C, M, H, W, 1, 1, 1, 1, 0)
+        self.l2 = Layer(batch, M, M, H, W, R1, R2, 3, stride, 1)
+        self.l3 = Layer(batch, M, C_out, self.l2.Ho, self.l2.Wo, 1, 1, 1, 1, 0)
+        self.lp = Layer(batch, C, C_out, H, W, 1, 1, 1, stride, 0) if self.projection else None
+        self.w = {k: torch.from_numpy(np.ascontiguousarray(v)).to(self.dev) for k, v in weights.items()}
+        norm = lambda L, act: GroupNorm(batch, L.Ho, L.Wo, L.N, math.gcd(groups, L.N), act=act, device=device)
+        new = lambda layer: torch.empty(layer.out_shape(), device=self.dev, dtype=torch.float32)
+        self.conv1, self.norm1 = MX4Conv2d(self.l1, device=device), norm(self.l1, "relu")
+        self.conv2, self.norm2 = TuckerConv2d(self.l2, device, tunings("tucker", self.l2, (False, False, False)) if tunings else None, layout=layout), norm(self.l2, "relu")
+        self.conv3, self.norm3 = MX4Conv2d(self.l3, device=device), norm(self.l3, "relu")
+        self.convp, self.normp = (MX4Conv2d(self.lp, device=device), norm(self.lp, "none")) if self.projection else (None, None)
+        self.conv1.pack(self.w["W1"])
+        self.conv2.pack(self.w["U_in"], self.w["core"], self.w["U_out"])
+        self.conv3.pack(self.w["W3"])
+        self.t1, self.t2, self.t3 = new(self.conv1), new(self.conv2), new(self.conv3)
+        self.n1, self.q2, self.y = torch.empty_like(self.t1), self.norm2.new_quantized(), torch.empty_like(self.t3)
+        self.tp = self.s = None
+        if self.projection:
+            self.convp.pack(self.w["Wp"])
+            self.tp, self.s = new(self.convp), torch.empty_like(self.y)
+        self._launchers = None
+        self._x = None
+
+    def bind(self, x):
+        self._x = x
+        weights = lambda k: dict(gamma=self.w["g" + k], beta=self.w["b" + k])
+        first = (self.convp.bind(x, self.tp), self.normp.bind(self.tp, self.s, **weights("p"))) if self.projection else ()
+        self._launchers = first + (
+            self.conv1.bind(x, self.t1),
+            self.norm1.bind(self.t1, self.n1, **weights("1")),
+            self.conv2.bind(self.n1, self.t2),
+            self.norm2.bind_quantized(self.t2, self.q2, **weights("2")),
+            self.conv3.bind(self.q2, self.t3),
+            self.norm3.bind(self.t3, self.y, residual=self.s if self.projection else x, **weights("3")),
+        )
+        return self
+
+    def _norms(self):
+        return [n for n in (self.normp, self.norm1, self.norm2, self.norm3) if n is not None]
+
+    def kernels(self) -> int:
+        # conv3 takes its rows quantised: one launch
+        return sum(n.kernel_count() for n in self._norms()) + sum(c.kernel_count() for c in self._convs() if c is not self.conv3) + 1
+
+    def describe(self) -> str:
+        head = "shortcut 1x1: 4 bits | " if self.projection else ""
+        return head + "1x1: 4 bits | 3x3: %s | 1x1: 4 bits | group norm: %s kernels" % (self.conv2.describe(), "+".join(str(n.kernel_count()) for n in self._norms()))
+
+    def close(self) -> None:
+        for c in self._convs() + self._norms():
+            c.close()
+
+
 def make_basic_weights(C: int, M: int, Ra: tuple, Rb: tuple, seed: int, projection: bool = False) -> Dict[str, np.ndarray]:
     """Seeded float32 weights of one basic block, N(0, 1/fan_in); biases N(0, 0.01).  Ra, Rb = (R1, R2) of the two layers."""
     rng = np.random.default_rng(seed)
@@ -234,11 +322,13 @@ class TuckerResNetBody:
     leaving with 4 M channels; the first block of a stage has a projection shortcut and, from the second stage on,
     stride 2 on its 3x3 convolution.  The input is the stem's output ([batch][width][H][W], 64 x 56 x 56 for the
     real network); the stem, pooling and classifier are dense layers outside this library.  Weights are seeded and
-    synthetic (make_block_weights), ranks come from ``rank(M)``."""
+    synthetic (make_block_weights), ranks come from ``rank(M)``.  ``norm``: blocks with group norm and 4-bit 1x1 weights
+    (TuckerNormBottleneck), channels last."""
 
     def __init__(self, batch: int, H: int = 56, W: int = 56, width: int = 64, blocks=(3, 4, 6, 3), rank=default_rank,
-                 seed: int = 0, device: int = 0, layout: int = B.LAYOUT_NCHW, tunings=None):
+                 seed: int = 0, device: int = 0, layout: int = B.LAYOUT_NCHW, tunings=None, norm: bool = False):
         import torch
+        make, block = (make_norm_block_weights, TuckerNormBottleneck) if norm else (make_block_weights, TuckerBottleneck)
         self.dev = torch.device("cuda", device)
         self.layout = layout
         self.batch, self.width = batch, width
@@ -251,8 +341,8 @@ class TuckerResNetBody:
                 first = i == 0
                 stride = 2 if (first and stage > 0) else 1
                 R = rank(M)
-                wts = make_block_weights(C, M, R, R, seed + 100 * stage + i, C_out=4 * M, projection=first)
-                blk = TuckerBottleneck(batch, C, M, h, w, R, R, wts, device, layout, stride=stride, C_out=4 * M, tunings=tunings)
+                wts = make(C, M, R, R, seed + 100 * stage + i, C_out=4 * M, projection=first)
+                blk = block(batch, C, M, h, w, R, R, wts, device, layout, stride=stride, C_out=4 * M, tunings=tunings)
                 assert blk.projection == first
                 self.blocks.append(blk)
                 self.weights.append(wts)
@@ -409,20 +499,25 @@ def main(argv=None) -> int:
         sys.exit("bottleneck needs a GPU")
     B.load()
     layout = B.LAYOUT_NHWC if argv and "--nhwc" in argv else B.LAYOUT_NCHW
+    if argv and "--norm" in argv and "--resnet50" not in argv:
+        sys.exit("--norm goes with --resnet50")
     if argv and ("--resnet50" in argv or "--resnet18" in argv):
         batch = int(argv[argv.index("--batch") + 1]) if "--batch" in argv else 1
         deep = "--resnet50" in argv
         cls = TuckerResNetBody if deep else TuckerResNet18Body
-        net = cls(batch, layout=layout)
+        norm = {"norm": True} if "--norm" in argv else {}
+        if norm:
+            layout = B.LAYOUT_NHWC
+        net = cls(batch, layout=layout, **norm)
         r = time_network(net)
         print(net.describe())
-        print("ResNet-%d body, batch %d, %s: %d blocks, %d kernels, %.3f GFLOP; eager %.1f us, one graph %.1f us" % (
-            50 if deep else 18, batch, "NHWC" if layout else "NCHW", len(net.blocks), net.kernels(), net.flops() / 1e9,
+        print("ResNet-%d body%s, batch %d, %s: %d blocks, %d kernels, %.3f GFLOP; eager %.1f us, one graph %.1f us" % (
+            50 if deep else 18, " with group norm and 4-bit 1x1 weights" if norm else "", batch, "NHWC" if layout else "NCHW", len(net.blocks), net.kernels(), net.flops() / 1e9,
             r["eager_us"], r["graph_us"]), flush=True)
         net.close()
         if "--oracle" in argv:       # the same network with every convolution's tuning found by exhaustive search
             pick, log = oracle_tunings(layout, progress=lambda m: print("   " + m, flush=True))
-            tuned = cls(batch, layout=layout, tunings=pick)
+            tuned = cls(batch, layout=layout, tunings=pick, **norm)
             ro = time_network(tuned)
             print(tuned.describe())
             print("... with exhaustively searched tunings (%d shapes searched): %d kernels; eager %.1f us, one graph %.1f us; "

@@ -207,7 +207,7 @@ int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_sc
     if (!a_codes || !a_scales || !b_codes || !b_scales || !y) return TDC_ERR_NULL;
     const int rc = check_epilogue(epilogue, dtype);
     if (rc != TDC_OK) return rc;
-    if (K > TDC_MX4_MAX_COLS || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
+    if (K > TDC_MX4_MAX_COLS || N > TDC_MX4_MAX_OUT || !tdc_aligned_to(a_codes, 16) || !tdc_aligned_to(b_codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     if (!tdc_mx4_product_fits(M, N)) return TDC_ERR_UNSUPPORTED;
     const TdcMx4Product q{a_codes, a_scales, b_codes, b_scales, M, N, tdc_mx4_blocks(K), TdcMx4Rows::all(), y, kernel_epilogue(epilogue), false};
     return tdc_launch_mx4_product(q, dtype, (hipStream_t)hip_stream) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
@@ -222,7 +222,7 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     if (s.x_pitch == 0) s.x_pitch = s.C;
     if (s.x_pitch < s.C) return TDC_ERR_BAD_SHAPE;
     const int64_t Ho = (s.H - 1) / s.stride + 1, Wo = (s.W - 1) / s.stride + 1, lim = 0x7fffffff;
-    if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS) return TDC_ERR_UNSUPPORTED;
+    if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS || s.N > TDC_MX4_MAX_OUT) return TDC_ERR_UNSUPPORTED;
     if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
     const int64_t rows = s.batch * Ho * Wo;
     if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 128)) return TDC_ERR_UNSUPPORTED;

@@ -77,6 +77,7 @@ hipError_t tdc_launch_mx4_lay_out(const uint8_t *codes, const uint8_t *scales, i
 hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, int dtype, const uint8_t *w, const uint8_t *ws, hipStream_t s, bool prepare_only = false);
 
 constexpr int TDC_MX4_MAX_COLS = 1 << 30;
+constexpr int TDC_MX4_MAX_OUT = 1 << 24;   // a lane's offset of some rows of y stays under 2^32 bytes
 
 // A convolution that the matrix cores bound rather than memory runs as quantisation and a product in large tiles.
 inline bool tdc_mx4_large(int64_t rows, int N, int K) { return rows >= 4096 && N >= 1024 && K >= 1024; }

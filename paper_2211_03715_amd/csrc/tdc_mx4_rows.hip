@@ -66,7 +66,7 @@ template <typename T, int E, typename Row> __device__ __forceinline__ void finis
 {
     if (n >= a.q.N) return;
     const bool two = n + 1 < a.q.N;
-    const unsigned lane = ((unsigned)(4 * h) * a.q.N + n) * sizeof(T);
+    const unsigned lane = ((unsigned)(4 * h) * a.q.N + n) * sizeof(T);   // N <= TDC_MX4_MAX_OUT
     if (a.q.epi.bias) {
         const float b0 = a.q.epi.bias[n], b1 = two ? a.q.epi.bias[n + 1] : 0.f;
 #pragma unroll
@@ -331,7 +331,7 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
     a.pairs = q.N % 2 == 0 && tdc_aligned_to(q.y, 2 * size) && tdc_aligned_to(q.epi.residual, 2 * size);
     const int64_t tiles = ((int64_t)q.M + 31) / 32;
     // Few tiles: a workgroup to 32 rows and 64 columns, eight wavefronts along k.  Many: the columns in turn, shared by as many
-    // workgroups as it takes to have two to a compute unit.
+    // workgroups as it takes to have four to a compute unit.
     const bool few = tdc_mx4_few(q.M, q.N) || !w;
     a.splits = few ? a.groups : (int)std::max<int64_t>(1, std::min<int64_t>((a.groups + 3) / 4, 1024 / tiles));
     // besides, KW = 1 stores through 18 KiB, KW = 8 adds up in 64 KiB where the codes were

@@ -115,3 +115,9 @@ def test_reference_norm_by_hand():
     pre, xhat, mean, rstd = R.group_norm(x, 2, 0.0)
     assert mean.tolist() == [[4, 11]] and torch.allclose(rstd, torch.tensor([[5.0 ** -.5, 3.0 ** -.5]], dtype=torch.float64))
     assert torch.allclose(xhat[0, 0, 0], torch.tensor([-3, -1, 0, 0], dtype=torch.float64) * rstd[0].repeat_interleave(2) + torch.tensor([0, 0, -1, -1]) * rstd[0, 1])
+
+
+def test_more_outputs_than_2_to_the_24_are_refused():
+    lib, plan = B.load(), ctypes.c_void_p()
+    assert lib.tdc_mx4_matmul(None, P, P, P, P, 1, (1 << 24) + 1, 32, P, 0, None) == B.TDC_ERR_UNSUPPORTED
+    assert lib.tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(_mx4(N=(1 << 24) + 1)), 0) == B.TDC_ERR_UNSUPPORTED and not plan.value
