@@ -22,17 +22,30 @@ struct NormIn {
     int act;                 // the same for every thread: a branch to V values costs next to nothing beside their way to memory
 };
 
-// Constants of a thread's V channels.
+// Constants of a thread's V channels: their weights, which can be on their way while the statistics are made, then all of it.
 template <int V> struct Affine {
     float mean[V], scale[V], shift[V];
+    __device__ __forceinline__ void weights(const NormIn &in, int c0)
+    {
+        // one branch to all of them: behind a branch of its own each load would wait by itself
+#pragma unroll
+        for (int v = 0; v < V; ++v) scale[v] = 1.f, shift[v] = 0.f;
+        if (in.gamma) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) scale[v] = in.gamma[c0 + v];
+        }
+        if (in.beta) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) shift[v] = in.beta[c0 + v];
+        }
+    }
     // stats: of the groups from g0 on
-    __device__ __forceinline__ void set(const TdcNormDims &d, const NormIn &in, const float2 *stats, int g0, int c0)
+    __device__ __forceinline__ void statistics(const TdcNormDims &d, const float2 *stats, int g0, int c0)
     {
         tdc_norm_channels<V>(c0, d.Cg, [&](int v, int g) {
             const float2 st = stats[g - g0];
             mean[v] = st.x;
-            scale[v] = in.gamma ? st.y * in.gamma[c0 + v] : st.y;
-            shift[v] = in.beta ? in.beta[c0 + v] : 0.f;
+            scale[v] *= st.y;
         });
     }
 };
@@ -95,37 +108,38 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
         if (out.mean) out.mean[at + g] = mean;
         if (out.rstd) out.rstd[at + g] = rstd;
     });
+    Affine<V> a;
+    a.weights(in, c0 + (live ? t.cv * V : 0));
     __syncthreads();
     if (!live && !MX4) return;
-    Affine<V> a;
-    a.set(d, in, stats, c0 / d.Cg, c0 + (live ? t.cv * V : 0));
+    a.statistics(d, stats, c0 / d.Cg, c0 + (live ? t.cv * V : 0));
     const T *res = in.residual ? static_cast<const T *>(in.residual) + (size_t)b * d.P * in.rp + c0 + t.cv * V : nullptr;
     // MX4: lanes that share a block have the same pixels, but their neighbours in the wavefront may have one less.  The residual
-    // comes four pixels at a time: behind a store, which might change it for all the compiler knows, each would wait by itself.
-    constexpr int R = HELD < 4 ? HELD : 4;
-#pragma unroll
-    for (int i0 = 0; i0 < HELD; i0 += R) {
-        if (i0 >= held_here) break;
-        TdcVec<T, V> rv[R];
-        if (res) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int p = tdc_anew(t.r + (i0 + i) * t.rows);
-                if (live && p < d.P) rv[i] = tdc_load<T, V>(res + (size_t)p * in.rp);
-            }
-        }
+    // comes R pixels at a time, one such step ahead of the stores: behind a store, which might change it for all the compiler
+    // knows, each of its loads would wait by itself.  Pieces of 8 leave no registers for that.
+    constexpr int R = V == 8 ? 1 : HELD < 4 ? HELD : 4, AHEAD = V == 8 ? 0 : R;
+    TdcVec<T, V> rv[V == 8 ? 1 : 2][R];
+    auto fetch = [&](int i0, TdcVec<T, V> (&to)[R]) {
+        if (!res || i0 >= held_here) return;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int p = tdc_anew(t.r + (i0 + i) * t.rows);
-            const bool mine = live && p < d.P;
-            if (MX4 ? i0 + i >= held_here : !mine) break;
-            tdc_forget(held[i0 + i]);
-            float o[V];
-            apply(a, held[i0 + i], rv[i], in, o);
-            const size_t px = (size_t)b * d.P + p;
-            if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
-            else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
+            if (live && p < d.P) to[i] = tdc_load<T, V>(res + (size_t)p * in.rp);
         }
+    };
+    if (AHEAD) fetch(0, rv[0]);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int p = tdc_anew(t.r + i * t.rows);
+        const bool mine = live && p < d.P;
+        if (MX4 ? i >= held_here : !mine) break;
+        if (i % R == 0 && i + AHEAD < HELD) fetch(i + AHEAD, rv[AHEAD ? i / R + 1 & 1 : 0]);
+        tdc_forget(held[i]);
+        float o[V];
+        apply(a, held[i], rv[AHEAD ? i / R & 1 : 0][i % R], in, o);
+        const size_t px = (size_t)b * d.P + p;
+        if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
+        else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
     }
 }
 
@@ -222,7 +236,8 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d
     if (t.r >= t.rows) return;
     for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
         Affine<V> a;
-        a.set(d, in, stats, 0, cv * V);
+        a.weights(in, cv * V);
+        a.statistics(d, stats, 0, cv * V);
         if (cv != t.cv) fetch(cv, t.r);
         for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
             float o[U][V];
@@ -261,7 +276,8 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply_blocks(TdcNor
             for (int v = 0; v < V; ++v) part[v] = 0.f;
             if (c0 + j < d.C) {                            // V divides C: all of them or none
                 Affine<V> a;
-                a.set(d, in, stats, 0, c0 + j);
+                a.weights(in, c0 + j);
+                a.statistics(d, stats, 0, c0 + j);
                 TdcVec<T, V> rv;
                 if (res) rv = tdc_load<T, V>(res + px * in.rp + c0 + j);
                 apply(a, tdc_load<T, V>(x + px * in.xp + c0 + j), rv, in, part);

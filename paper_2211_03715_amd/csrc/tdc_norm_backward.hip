@@ -26,10 +26,16 @@ template <int V> struct Channels {
     float mean[V], rstd[V], gamma[V], beta[V];
     __device__ __forceinline__ void weights(const GradIn &q, int c0)
     {
+        // one branch to all of them: behind a branch of its own each load would wait by itself
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            gamma[v] = q.gamma ? q.gamma[c0 + v] : 1.f;
-            beta[v] = q.beta ? q.beta[c0 + v] : 0.f;
+        for (int v = 0; v < V; ++v) gamma[v] = 1.f, beta[v] = 0.f;
+        if (q.gamma) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) gamma[v] = q.gamma[c0 + v];
+        }
+        if (q.beta) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) beta[v] = q.beta[c0 + v];
         }
     }
     __device__ __forceinline__ void statistics(const TdcNormDims &d, const GradIn &q, int b, int c0)
