@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void tdc_mx4_dequantize_lanes(const uint8_t *_
         tdc_mx4_values(c[u], e[u], v);
         T *out = y + m * pitch + c0;
         if constexpr (VECTORS) {
-            if (c0 < cols) tdc_store<T, V>(out, v);
+            if (c0 < cols) tdc_store_stream<T, V>(out, v);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)

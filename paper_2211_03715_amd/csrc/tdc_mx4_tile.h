@@ -56,7 +56,8 @@ template <typename T, int V> __device__ __forceinline__ void tdc_mx4_finish(cons
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = tdc_activate<TDC_ACT_SILU>(v[i]);
     }
-    tdc_store<T, V>(static_cast<T *>(q.y) + at, v);
+    // y is not read again; 56x56x256 -> 512 of every second pixel, 32 images in fp32: 18.6 us with ordinary stores, 15.8 so
+    tdc_store_stream<T, V>(static_cast<T *>(q.y) + at, v);
 }
 
 // `rows` x `cols` sums that a wavefront holds in LDS, `pitch` floats to a row, into y from (m0, n0) on.

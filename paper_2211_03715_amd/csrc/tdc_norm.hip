@@ -13,6 +13,7 @@ struct NormOut {
     uint8_t *codes, *scales;
     int64_t pitch;
     float *mean, *rstd;      // or null
+    bool stream;             // how y is stored
 };
 
 struct NormIn {
@@ -60,6 +61,12 @@ __device__ __forceinline__ void apply(const Affine<V> &k, const TdcVec<T, V> &x,
         for (int v = 0; v < V; ++v) o[v] += (float)res.v[v];
     }
     tdc_activate_all(in.act, o);
+}
+
+template <typename T, int V> __device__ __forceinline__ void store(const NormOut &out, T *p, const float (&o)[V])
+{
+    if (out.stream) tdc_store_stream<T, V>(p, o);
+    else tdc_store<T, V>(p, o);
 }
 
 // V of a block's 32 channels to a lane, 32 / V neighbouring lanes to a block: all of them call this, `live` or not.
@@ -139,7 +146,7 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
         apply(a, held[i], rv[AHEAD ? i / R & 1 : 0][i % R], in, o);
         const size_t px = (size_t)b * d.P + p;
         if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
-        else tdc_store<T, V>(static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
+        else store(out, static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
     }
 }
 
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d
             for (int u = 0; u < U; ++u) {
                 const int p = p0 + u * t.rows;
                 if constexpr (MX4) store_mx4<V>(out, o[u], first + p, (d.C + 31) / 32, cv * V, p < len);
-                else if (p < len) tdc_store<T, V>(static_cast<T *>(out.y) + (first + p) * out.pitch + cv * V, o[u]);
+                else if (p < len) store(out, static_cast<T *>(out.y) + (first + p) * out.pitch + cv * V, o[u]);
             }
         }
         if (t.rows > 1) break;
@@ -390,11 +397,11 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     DeviceGuard guard(p->device);
     if (!guard.ok) return TDC_ERR_HIP;
     const NormIn in{x, a.residual, gamma, beta, xp, rp, p->shape.act};
-    const NormOut out{y, codes, scales, yp, a.mean, a.rstd};
     const int vx = tdc_norm_vec(dt, d.C, {xp}, {x});
     const int V0 = y ? tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0, yp}, {x, a.residual, y}) : tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0}, {x, a.residual});
     const bool lanes = codes && d.C % 32 == 0 && V0 * size == 16;     // blocks of 4-bit values over neighbouring lanes
     const TdcNormSlice sl = y || lanes ? tdc_norm_slice(d, dt, V0, false, lanes ? 32 : 1) : TdcNormSlice{};
+    const NormOut out{y, codes, scales, yp, a.mean, a.rstd, y && tdc_norm_streams(d, dt, V0, sl)};
     const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);
     if (sl.held) {

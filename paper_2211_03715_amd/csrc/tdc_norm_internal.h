@@ -397,6 +397,16 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool 
     return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
 }
 
+// Whether the forward kernels store y past the L2's replacement: where workgroups write half lines or more of a tensor larger
+// than an XCD's L2 at about the same time, in pieces of 8 bytes or more.  28x28x512 in bf16, 32 images, 64 bytes to a slice: 18.4
+// us otherwise, 14.6 so.  But 56x56x256 in fp32, 32 images, where a compute unit has one workgroup of 1024 threads, with 64 bytes
+// to a slice 38.5 otherwise, 47.7 so; 56x56x64 in fp32, one image: 7.9 and 8.3.
+inline bool tdc_norm_streams(const TdcNormDims &d, int dtype, int V, const TdcNormSlice &sl)
+{
+    const int size = tdc_dtype_bytes(dtype);
+    return sl.threads != 1024 && (sl.held ? sl.width : d.C) * size >= 64 && V * size >= 8 && (double)d.B * d.P * d.C * size > 4e6;
+}
+
 // Workgroup id -> (image, slice): the ids that one XCD gets, 8 apart, are neighbours.
 __device__ __forceinline__ void tdc_norm_place(int id, int total, int slices, int &b, int &slice)
 {

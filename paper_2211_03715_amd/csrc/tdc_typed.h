@@ -55,6 +55,23 @@ template <typename T, int V> __device__ __forceinline__ void tdc_store(T *p, con
     *reinterpret_cast<TdcVec<T, V> *>(p) = o;
 }
 
+// The same past the L2's replacement: for results that fill whole lines at a time and are not read again by this kernel, which
+// then has less to write back when it ends.
+template <typename T, int V> __device__ __forceinline__ void tdc_store_stream(T *p, const float (&f)[V])
+{
+    TdcVec<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = (T)f[i];
+    if constexpr (sizeof(o) >= 4) {
+        typedef unsigned Words __attribute__((ext_vector_type(sizeof(o) / 4)));
+        Words w;
+        __builtin_memcpy(&w, &o, sizeof(o));
+        __builtin_nontemporal_store(w, reinterpret_cast<Words *>(p));
+    } else {
+        *reinterpret_cast<TdcVec<T, V> *>(p) = o;
+    }
+}
+
 // 1 / (1 + exp(-v)): v_exp and v_rcp are good to about an ulp each, and both ends are right: exp(-v) = inf gives 0, 0 gives 1.
 __device__ __forceinline__ float tdc_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
