@@ -97,14 +97,17 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
     const TdcNormLanes t(nv, THREADS);
     const bool live = t.r < min(t.rows, d.P) && t.cv < nv;
     const T *x = static_cast<const T *>(in.x) + (size_t)b * d.P * in.xp + c0 + t.cv * V;
-    TdcVec<T, V> held[HELD];
+    TdcRaw<T, V> held[HELD];
     TdcNormSums<V, WHOLE> sums;
     if (live) {
         // held_here is the same for all threads: what lies behind it is skipped without a load
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
-            if (i < held_here) held[i] = tdc_load<T, V>(x + (size_t)min(t.r + i * t.rows, d.P - 1) * in.xp);
-        sums.add(held, (d.P - t.r + t.rows - 1) / t.rows);
+            if (i < held_here) held[i].load(x + (size_t)min(t.r + i * t.rows, d.P - 1) * in.xp);
+        TdcVec<T, V> v[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) v[i] = held[i].open();
+        sums.add(v, (d.P - t.r + t.rows - 1) / t.rows);
     }
     const int rows = tdc_norm_put<V, WHOLE, THREADS>(items, sums, t, t.cv, nv, live, min(t.rows, d.P));
     __syncthreads();
@@ -125,13 +128,13 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
     // comes R pixels at a time, one such step ahead of the stores: behind a store, which might change it for all the compiler
     // knows, each of its loads would wait by itself.  Pieces of 8 leave no registers for that.
     constexpr int R = V == 8 ? 1 : HELD < 4 ? HELD : 4, AHEAD = V == 8 ? 0 : R;
-    TdcVec<T, V> rv[V == 8 ? 1 : 2][R];
-    auto fetch = [&](int i0, TdcVec<T, V> (&to)[R]) {
+    TdcRaw<T, V> rv[V == 8 ? 1 : 2][R];
+    auto fetch = [&](int i0, TdcRaw<T, V> (&to)[R]) {
         if (!res || i0 >= held_here) return;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int p = tdc_anew(t.r + (i0 + i) * t.rows);
-            if (live && p < d.P) to[i] = tdc_load<T, V>(res + (size_t)p * in.rp);
+            if (live && p < d.P) to[i].load(res + (size_t)p * in.rp);
         }
     };
     if (AHEAD) fetch(0, rv[0]);
@@ -141,9 +144,8 @@ __global__ __launch_bounds__(THREADS, 4) void tdc_norm_resident(TdcNormDims d, N
         const bool mine = live && p < d.P;
         if (MX4 ? i >= held_here : !mine) break;
         if (i % R == 0 && i + AHEAD < HELD) fetch(i + AHEAD, rv[AHEAD ? i / R + 1 & 1 : 0]);
-        tdc_forget(held[i]);
         float o[V];
-        apply(a, held[i], rv[AHEAD ? i / R & 1 : 0][i % R], in, o);
+        apply(a, held[i].open(), rv[AHEAD ? i / R & 1 : 0][i % R].open(), in, o);
         const size_t px = (size_t)b * d.P + p;
         if constexpr (MX4) store_mx4<V>(out, o, px, (d.C + 31) / 32, c0 + t.cv * V, mine);
         else store(out, static_cast<T *>(out.y) + px * out.pitch + c0 + t.cv * V, o);
@@ -227,29 +229,34 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_apply(TdcNormDims d
     const TdcNormLanes t(nv, TDC_NORM_THREADS);
     const size_t first = (size_t)b * d.P + (size_t)chunk * d.chunk_px;
     const T *x = static_cast<const T *>(in.x) + first * in.xp, *res = in.residual ? static_cast<const T *>(in.residual) + first * in.rp : nullptr;
-    TdcVec<T, V> v[U], rv[U];
+    TdcRaw<T, V> v[U], rv[U];
     auto fetch = [&](int cv, int p0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = tdc_load<T, V>(x + (size_t)min(p0 + u * t.rows, len - 1) * in.xp + cv * V);
+        for (int u = 0; u < U; ++u) v[u].load(x + (size_t)min(p0 + u * t.rows, len - 1) * in.xp + cv * V);
         if (res) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) rv[u] = tdc_load<T, V>(res + (size_t)min(p0 + u * t.rows, len - 1) * in.rp + cv * V);
+            for (int u = 0; u < U; ++u) rv[u].load(res + (size_t)min(p0 + u * t.rows, len - 1) * in.rp + cv * V);
         }
     };
-    // the first pixels are on their way while the statistics are put together
-    if (t.r < t.rows && t.cv < nv) fetch(t.cv, t.r);
+    // the first pixels and the weights are on their way while the statistics are put together
+    Affine<V> a;
+    if (t.r < t.rows && t.cv < nv) {
+        fetch(t.cv, t.r);
+        a.weights(in, t.cv * V);
+    }
     statistics(d, out, partial, parts, b, chunk, stats);
     // MX4: the lanes of a block go through the loops together (nv is a multiple of 32 / V)
     if (t.r >= t.rows) return;
     for (int cv = t.cv; cv < nv; cv += TDC_NORM_THREADS) {
-        Affine<V> a;
-        a.weights(in, cv * V);
+        if (cv != t.cv) {
+            fetch(cv, t.r);
+            a.weights(in, cv * V);
+        }
         a.statistics(d, stats, 0, cv * V);
-        if (cv != t.cv) fetch(cv, t.r);
         for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
             float o[U][V];
 #pragma unroll
-            for (int u = 0; u < U; ++u) apply(a, v[u], rv[u], in, o[u]);
+            for (int u = 0; u < U; ++u) apply(a, v[u].open(), rv[u].open(), in, o[u]);
             if (p0 + t.rows * U < len) fetch(cv, p0 + t.rows * U);
 #pragma unroll
             for (int u = 0; u < U; ++u) {

@@ -216,26 +216,26 @@ __global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d,
         const size_t first_px = (size_t)image * d.P;
         const T *px = static_cast<const T *>(q.x) + first_px * q.xp + c0, *pdy = static_cast<const T *>(q.dy) + first_px * q.dyp + c0;
         const T *pres = has_res ? static_cast<const T *>(q.residual) + first_px * q.rp + c0 : nullptr;
-        TdcVec<T, V> x[HELD];
+        TdcRaw<T, V> x[HELD];
         float dd[HELD][V], s1[V], s2[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) s1[v] = s2[v] = 0.f;
         if (live) {
-            TdcVec<T, V> dy[HELD], res[HELD];
+            TdcRaw<T, V> dy[HELD], res[HELD];
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
                 if (i < held_here) {
                     const int p = tdc_anew(min(t.r + i * t.rows, d.P - 1));
-                    x[i] = tdc_load<T, V>(px + (size_t)p * q.xp);
-                    dy[i] = tdc_load<T, V>(pdy + (size_t)p * q.dyp);
-                    if (has_res) res[i] = tdc_load<T, V>(pres + (size_t)p * q.rp);
+                    x[i].load(px + (size_t)p * q.xp);
+                    dy[i].load(pdy + (size_t)p * q.dyp);
+                    if (has_res) res[i].load(pres + (size_t)p * q.rp);
                 }
             k.statistics(d, q, image, c0);
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
                 if (t.r + i * t.rows < d.P) {
                     float xhat[V];
-                    gradient(k, x[i], dy[i], res[i], q, dd[i], xhat);
+                    gradient(k, x[i].open(), dy[i].open(), res[i].open(), q, dd[i], xhat);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         s1[v] += dd[i][v];
@@ -262,10 +262,10 @@ __global__ __launch_bounds__(THREADS) void tdc_norm_grad_resident(TdcNormDims d,
             for (int i = 0; i < HELD; ++i) {
                 const int p = tdc_anew(t.r + i * t.rows);
                 if (p >= d.P) break;
-                tdc_forget(x[i]);
+                const TdcVec<T, V> xv = x[i].open();
                 float xhat[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) xhat[v] = ((float)x[i].v[v] - k.mean[v]) * k.rstd[v];
+                for (int v = 0; v < V; ++v) xhat[v] = ((float)xv.v[v] - k.mean[v]) * k.rstd[v];
                 store_gradients<T, V>(k, out, m1, m2, dd[i], xhat, first_px + p, c0);
             }
         }
@@ -301,19 +301,19 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDi
             if (live) {
                 k.statistics(d, q, b, cv * V);
                 for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
-                    TdcVec<T, V> xv[U], dv[U], rv[U];
+                    TdcRaw<T, V> xv[U], dv[U], rv[U];
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         const size_t px = first + min(p0 + u * t.rows, len - 1);
-                        xv[u] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + cv * V);
-                        dv[u] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
-                        if (res) rv[u] = tdc_load<T, V>(res + px * q.rp + cv * V);
+                        xv[u].load(static_cast<const T *>(q.x) + px * q.xp + cv * V);
+                        dv[u].load(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
+                        if (res) rv[u].load(res + px * q.rp + cv * V);
                     }
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         if (p0 + u * t.rows >= len) break;
                         float dd[V], xhat[V];
-                        gradient(k, xv[u], dv[u], rv[u], q, dd, xhat);
+                        gradient(k, xv[u].open(), dv[u].open(), rv[u].open(), q, dd, xhat);
 #pragma unroll
                         for (int v = 0; v < V; ++v) {
                             s1[v] += dd[v];
@@ -379,19 +379,19 @@ __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_apply(TdcNormD
             m2[v] = means[g].y;
         });
         for (int p0 = t.r; p0 < len; p0 += t.rows * U) {
-            TdcVec<T, V> xv[U], dv[U], rv[U];
+            TdcRaw<T, V> xv[U], dv[U], rv[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const size_t px = first + min(p0 + u * t.rows, len - 1);
-                xv[u] = tdc_load<T, V>(static_cast<const T *>(q.x) + px * q.xp + cv * V);
-                dv[u] = tdc_load<T, V>(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
-                if (res) rv[u] = tdc_load<T, V>(res + px * q.rp + cv * V);
+                xv[u].load(static_cast<const T *>(q.x) + px * q.xp + cv * V);
+                dv[u].load(static_cast<const T *>(q.dy) + px * q.dyp + cv * V);
+                if (res) rv[u].load(res + px * q.rp + cv * V);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (p0 + u * t.rows >= len) break;
                 float dd[V], xhat[V];
-                gradient(k, xv[u], dv[u], rv[u], q, dd, xhat);
+                gradient(k, xv[u].open(), dv[u].open(), rv[u].open(), q, dd, xhat);
                 store_gradients<T, V>(k, out, m1, m2, dd, xhat, first + p0 + u * t.rows, cv * V);
             }
         }

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "tdc_internal.h"
 #include "tdc_norm.h"
 
@@ -27,18 +29,29 @@ template <typename T, int V> __device__ __forceinline__ TdcVec<T, V> tdc_load(co
     return *reinterpret_cast<const TdcVec<T, V> *>(p);
 }
 
-// Makes the compiler take `x` for something new, so that what it computed from x before is computed again and not kept: a
-// kernel that goes twice over pieces in registers has no room for both the pieces and their values.
-template <typename T, int V> __device__ __forceinline__ void tdc_forget(TdcVec<T, V> &x)
-{
-    if constexpr (sizeof(T) * V >= 4) {
-        unsigned w[sizeof(T) * V / 4];
-        __builtin_memcpy(w, &x, sizeof(w));
-#pragma unroll
-        for (unsigned &u : w) asm volatile("" : "+v"(u));
-        __builtin_memcpy(&x, w, sizeof(w));
+// V neighbours as the words they are loaded as, for pieces that are held or fetched ahead.  Elements of TdcVec that live across a
+// branch become values of their own to the compiler, and those of 16 bits are cut out of their words, and waited for, right behind
+// the load: one load after the other.
+template <typename T, int V> struct TdcRaw {
+    static constexpr int BYTES = sizeof(T) * V;
+    typedef unsigned Vector __attribute__((ext_vector_type(BYTES < 8 ? 2 : BYTES / 4)));
+    typedef std::conditional_t<BYTES < 8, unsigned, Vector> Words;
+    Words w;
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (BYTES < 4) w = *reinterpret_cast<const unsigned short *>(p);
+        else w = *reinterpret_cast<const Words *>(p);
     }
-}
+    // The neighbours, made anew: the compiler takes them for something it has not seen, so that what it computed from them before is
+    // computed again and not kept.  A kernel that goes twice over pieces in registers has no room for both the pieces and their values.
+    __device__ __forceinline__ TdcVec<T, V> open()
+    {
+        asm volatile("" : "+v"(w));
+        TdcVec<T, V> o;
+        __builtin_memcpy(&o, &w, BYTES);
+        return o;
+    }
+};
 
 // The same for an index, whose addresses are then made where they are used and do not fill registers until then.
 __device__ __forceinline__ int tdc_anew(int i)
