@@ -17,23 +17,27 @@ __global__ __launch_bounds__(256) void tdc_mx4_quantize_lanes(const T *__restric
     const int lane = threadIdx.x & (LANES - 1);
     const int64_t first = (int64_t)blockIdx.x * (256 * U / LANES) + threadIdx.x / LANES;
     float v[U][V];
+    TdcRaw<T, V> in[U];
+    int c0[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t i = min(first + u * (256 / LANES), total - 1), m = blocks.of(i);
-        const int c0 = (int)(i - m * blocks.d) * 32 + lane * V;
-        const T *p = x + rows.source(m) * pitch + c0;
+        c0[u] = (int)(i - m * blocks.d) * 32 + lane * V;
+        const T *p = x + rows.source(m) * pitch + c0[u];
         if constexpr (VECTORS) {
-            TdcVec<T, V> in;
-            if (c0 < cols) in = tdc_load<T, V>(p);             // V divides cols: all of them or none
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[u][j] = c0 < cols ? (float)in.v[j] : 0.f;
+            if (c0[u] < cols) in[u].load(p);                   // V divides cols: all of them or none
         } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[u][j] = c0 + j < cols ? (float)p[j] : 0.f;
+            for (int j = 0; j < V; ++j) v[u][j] = c0[u] + j < cols ? (float)p[j] : 0.f;
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        if constexpr (VECTORS) {
+            const TdcVec<T, V> o = in[u].open();
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[u][j] = c0[u] < cols ? (float)o.v[j] : 0.f;
+        }
         unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) top = max(top, tdc_abs_bits(v[u][j]));

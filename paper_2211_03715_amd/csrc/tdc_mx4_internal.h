@@ -16,9 +16,8 @@ struct TdcMx4Rows {
     __host__ __device__ int64_t source(int64_t m) const
     {
         if (stride == 1) return m;
-        const int64_t b = m / HoWo;
-        const int q = (int)(m - b * HoWo), i = q / Wo, j = q - i * Wo;
-        return b * HW + (int64_t)i * stride * W + (int64_t)j * stride;
+        const int b = (int)m / HoWo, q = (int)m - b * HoWo, i = q / Wo, j = q - i * Wo;    // a plan's pixels are under 2^31
+        return (int64_t)b * HW + (int64_t)i * stride * W + (int64_t)j * stride;
     }
 };
 
