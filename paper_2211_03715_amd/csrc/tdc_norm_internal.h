@@ -386,7 +386,7 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool 
     };
     auto fits = [&](int width) { return held(width, 512) <= most; };
     auto groups = [&](int width) { return (int64_t)d.B * (d.C / width); };
-    if (!fits(unit)) return TdcNormSlice{0, 0, 0, 0};
+    if (!fits(unit)) return TdcNormSlice{};
     int width = unit;
     for (int w = next(width); w <= d.C && (width * size < 64 || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
     if (!backward && width * size < 64 && (int64_t)d.B * d.P * d.C * size > (32 << 20)) {
@@ -394,6 +394,7 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool 
         if (w <= d.C && held(w, 1024) <= most) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
     }
     const int threads = held(width, 256) <= 4 ? 256 : 512;
+    if (!backward && groups(width) * threads > 0xffffffffll) return TdcNormSlice{};   // a launch counts its threads in 32 bits
     return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
 }
 

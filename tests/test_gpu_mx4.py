@@ -311,3 +311,18 @@ def test_refusals_of_the_layer():
     with pytest.raises(ValueError):
         mx4.matmul(a, a, 64, dtype=torch.float64)
     assert mx4.matmul(tuple(t[:0].contiguous() for t in a), a, 64).shape == (0, 32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pitch", [(7, 64, 96), (5, 33, 40), (300, 24, 25), (1, 5, 9)])
+def test_values_written_apart(rows, cols, pitch, dtype):
+    """tdc_mx4_dequantize with a pitch: what lies between the rows stays as it was."""
+    from paper_2211_03715_amd import binding as B
+    x = torch.randn((rows, cols), generator=_gen(rows)).to(dtype)
+    codes, scales = R.quantize(x)
+    wide = torch.full((rows, pitch), 7.0, dtype=dtype, device="cuda")
+    c, s = codes.cuda(), scales.cuda()
+    code = {F32: 0, BF16: 2}[dtype]
+    assert B.load().tdc_mx4_dequantize(torch.cuda.current_stream().cuda_stream, c.data_ptr(), s.data_ptr(), rows, cols, wide.data_ptr(), code, pitch) == B.TDC_OK
+    wide = wide.cpu()
+    assert torch.equal(wide[:, :cols].double(), R.values(codes, scales, cols).to(dtype).double()) and bool((wide[:, cols:] == 7).all())

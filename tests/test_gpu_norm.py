@@ -298,3 +298,15 @@ def test_refusals_of_the_layer():
         GroupNorm(1, 1, 1, 8, 2, act="gelu")
     with pytest.raises(ValueError):
         GroupNorm(1, 1, 1, 8, 2, dtype=torch.float64)
+
+
+def test_more_slices_than_a_launch_has_threads_for():
+    """65535 images of one pixel, 8144 = 16 * 509 channels in 509 groups: slices of 16 channels would need 2^33 threads."""
+    B, C, G = 65535, 8144, 509
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.empty((B, 1, 1, C), device="cuda", dtype=BF16).normal_(generator=g)
+    gn = _layer(B, 1, 1, C, G, "relu", BF16)
+    y = gn(x)
+    some = torch.tensor([0, 1, 255, 30000, B - 2, B - 1], device="cuda")
+    _check_forward(y[some], x[some].cpu(), G, "relu", BF16, None, None, None, "y")
+    del x, y
