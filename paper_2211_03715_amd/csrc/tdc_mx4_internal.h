@@ -85,8 +85,8 @@ inline bool tdc_mx4_large(int64_t rows, int N, int K) { return rows >= 4096 && N
 inline bool tdc_mx4_few(int64_t rows, int N) { return (rows + 31) / 32 * ((N + 63) / 64) <= 512; }
 
 // Every one of those quantises its rows of x anew, which takes longer than a launch where they have over 192 KB: 64 rows,
-// 4096 -> 4096 in bf16 (262 KB) 18.5 us, with x quantised in a launch of its own 10.3; 1568 rows, 2048 -> 512 in fp32 (262 KB)
-// 21.3 and 15.1; 6272 rows, 512 -> 128 in fp32 (66 KB) 7.8 and 11.0.
+// 4096 -> 4096 in bf16 (262 KB) 17.4 us, with x quantised in a launch of its own 10.4; 1568 rows, 2048 -> 512 in fp32 (262 KB)
+// 21.1 and 13.7; 6272 rows, 512 -> 128 in fp32 (66 KB) 7.4 and 10.0.
 inline bool tdc_mx4_quantise_first(int64_t rows, int N, int K, int size) { return tdc_mx4_few(rows, N) && (double)(rows < 32 ? rows : 32) * K * size > 192e3; }
 
 #endif  // TDC_MX4_INTERNAL_H

@@ -315,8 +315,8 @@ int validate(const tdc_norm_shape &s)
 }
 
 // Pixels to a chunk: four workgroups to a compute unit over the batch, but four pieces to a thread, since what a thread does once,
-// for its channels and for its sums, costs as much as some pieces (224x224x64 in fp16: 20.8 us with two, 16.1 with four); two or
-// one where that leaves compute units without work (37x29x150 in bf16, 3 images: 13.1 us with four, 11.2 with two).
+// for its channels and for its sums, costs as much as some pieces (224x224x64 in fp16: 17.8 us with two, 14.6 with four); two or
+// one where that leaves compute units without work (37x29x150 in bf16, 3 images: 12.7 us with four, 10.8 with two, 9.6 with one).
 void choose_chunks(TdcNormDims &d, int dtype)
 {
     const int pieces = (d.C * tdc_dtype_bytes(dtype) + 15) / 16;

@@ -20,7 +20,7 @@ constexpr int TDC_NORM_THREADS = 512;    // of the kernels that run over chunks
 constexpr int TDC_NORM_MAX_C = 8192;     // per-channel pairs of a workgroup fill at most 64 KiB of LDS
 constexpr int TDC_NORM_UNROLL = 4;       // pixels that a thread has in flight
 // Chunks of an image that every workgroup of the second kernel combines for itself.  More than that are combined by a kernel in
-// between: 224x224x64 in fp16, 196 chunks, 18.2 us without it and 16.1 with it; at 64 chunks the two are even.
+// between: 224x224x64 in fp16, 196 chunks, 16.5 us without it and 14.3 with it; at 64 chunks the two are even.
 constexpr int TDC_NORM_PARTS = 64;
 
 struct TdcNormDims {
@@ -363,15 +363,17 @@ struct TdcNormSlice {
     int width, slices, threads, held;    // held: pieces to a thread; 0: the image does not fit
 };
 
-// The narrowest slices (whole groups, whole pieces, multiples of `multiple`) are widened to 64 bytes of a pixel, and until there
-// are no more than 1024 of them, as long as 512 threads hold them and 256 workgroups are left.  A line that several workgroups
-// share comes from memory once all the same: they run on the same XCD (tdc_norm_place).  Measured, forward, fp32, 28x28x512, 32
-// images: 16 channels 20.4 us, 32 20.0, 64 22.5; 28x28x128 in bf16: 8 channels 12.4, 16 9.9, 32 11.6; 7x7x512, 256 images: 16
-// channels 25 us, 64 18, 128 16.4.  1024 threads lose everywhere (no second workgroup that reads while one writes) but where
-// slices below 64 bytes of a tensor larger than the L2s can be wider by them: 56x56x256, 32 images: 8 channels 42.4 us, 16 40.2.
+// The narrowest slices (whole groups, whole pieces, multiples of `multiple`) are widened to a line of 128 bytes of a pixel, or 64
+// backward, and until there are no more than 1024 of them, as long as 512 threads hold them and 256 workgroups are left.  A line
+// that several workgroups share comes from memory once all the same: they run on the same XCD (tdc_norm_place).  Measured,
+// forward, fp32, 28x28x512, 32 images: 16 channels 21.8 us, 32 17.8; 28x28x128 in bf16, 32 images: 8 channels 9.6, 16 8.8, 32,
+// with 128 workgroups, 9.8; 7x7x512, 256 images: 16 channels 30.9 us, 64 and 128 11.9.  Backward, 14x14x1024 in bf16, 32 images:
+// 64 bytes 16.5, 128 18.9.  1024 threads lose everywhere (28x28x512, 32 images, 32 channels: 26.5; no second workgroup that reads
+// while one writes) but where slices below 64 bytes of a tensor larger than the L2s can be wider by them: 56x56x256, 32 images:
+// 8 channels 41.5 us, 16 38.9.
 inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool backward, int multiple)
 {
-    const int most = tdc_norm_held(V, tdc_dtype_bytes(dtype), backward), size = tdc_dtype_bytes(dtype);
+    const int size = tdc_dtype_bytes(dtype), most = tdc_norm_held(V, size, backward), line = backward ? 64 : 128;
     int unit = d.Cg;
     while ((unit % V || unit % multiple) && unit < d.C) unit += d.Cg;
     if (unit > d.C || d.C % unit) unit = d.C;
@@ -388,7 +390,7 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool 
     auto groups = [&](int width) { return (int64_t)d.B * (d.C / width); };
     if (!fits(unit)) return TdcNormSlice{};
     int width = unit;
-    for (int w = next(width); w <= d.C && (width * size < 64 || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
+    for (int w = next(width); w <= d.C && (width * size < line || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
     if (!backward && width * size < 64 && (int64_t)d.B * d.P * d.C * size > (32 << 20)) {
         const int w = next(width);
         if (w <= d.C && held(w, 1024) <= most) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
