@@ -314,24 +314,6 @@ int validate(const tdc_norm_shape &s)
     return TDC_OK;
 }
 
-// Pixels to a chunk: four workgroups to a compute unit over the batch, but four pieces to a thread, since what a thread does once,
-// for its channels and for its sums, costs as much as some pieces (224x224x64 in fp16: 17.8 us with two, 14.6 with four); two or
-// one where that leaves compute units without work (37x29x150 in bf16, 3 images: 12.7 us with four, 10.8 with two, 9.6 with one).
-void choose_chunks(TdcNormDims &d, int dtype)
-{
-    const int pieces = (d.C * tdc_dtype_bytes(dtype) + 15) / 16;
-    const int rows = pieces < TDC_NORM_THREADS ? TDC_NORM_THREADS / pieces : 1;
-    const int most = d.B >= 1024 ? 1 : 1024 / d.B;
-    int64_t chunks = 1;
-    for (int each = 4; each; each /= 2) {
-        chunks = ((int64_t)d.P + each * rows - 1) / (each * rows);
-        if (d.B * chunks >= 128) break;
-    }
-    chunks = std::min<int64_t>(most, chunks);
-    d.chunk_px = (int)((d.P + chunks - 1) / chunks);
-    d.chunks = (d.P + d.chunk_px - 1) / d.chunk_px;
-}
-
 int64_t pitch_or(int64_t pitch, int C) { return pitch ? pitch : C; }
 
 }  // namespace
@@ -353,7 +335,7 @@ int tdc_norm_plan_create(tdc_norm_plan **out, const tdc_norm_shape *shape, int d
     p->shape = *shape;
     p->device = device;
     p->dims = TdcNormDims{shape->batch, shape->H * shape->W, shape->C, shape->groups, shape->C / shape->groups, 0, 0, shape->eps};
-    choose_chunks(p->dims, shape->dtype);
+    tdc_norm_choose_chunks(p->dims, tdc_dtype_bytes(shape->dtype));
     const size_t groups = (size_t)p->dims.B * p->dims.G, partials = groups * p->dims.chunks;
     const size_t sums = tdc_norm_sum_rows(p->dims) * p->dims.C;
     p->ws_bytes = (partials + groups) * sizeof(float4) + sums * sizeof(float2);
@@ -383,7 +365,7 @@ int tdc_norm_plan_kernel_count(const tdc_norm_plan *p)
 {
     if (!p) return 0;
     const int V = tdc_norm_vec(p->shape.dtype, p->dims.C, {}, {});
-    return tdc_norm_slice(p->dims, p->shape.dtype, V, false, 1).held ? 1 : p->dims.chunks > TDC_NORM_PARTS ? 3 : 2;
+    return tdc_norm_slice(p->dims, tdc_dtype_bytes(p->shape.dtype), V, false, 1).held ? 1 : p->dims.chunks > TDC_NORM_PARTS ? 3 : 2;
 }
 
 }  // extern "C"
@@ -407,8 +389,8 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     const int vx = tdc_norm_vec(dt, d.C, {xp}, {x});
     const int V0 = y ? tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0, yp}, {x, a.residual, y}) : tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0}, {x, a.residual});
     const bool lanes = codes && d.C % 32 == 0 && V0 * size == 16;     // blocks of 4-bit values over neighbouring lanes
-    const TdcNormSlice sl = y || lanes ? tdc_norm_slice(d, dt, V0, false, lanes ? 32 : 1) : TdcNormSlice{};
-    const NormOut out{y, codes, scales, yp, a.mean, a.rstd, y && tdc_norm_streams(d, dt, V0, sl)};
+    const TdcNormSlice sl = y || lanes ? tdc_norm_slice(d, size, V0, false, lanes ? 32 : 1) : TdcNormSlice{};
+    const NormOut out{y, codes, scales, yp, a.mean, a.rstd, y && tdc_norm_streams(d, size, V0, sl)};
     const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);
     if (sl.held) {

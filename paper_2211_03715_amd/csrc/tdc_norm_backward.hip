@@ -423,7 +423,7 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
     float2 *sums = weight_blocks ? p->sums : nullptr;
     const int vec = tdc_norm_vec(dt, d.C, {q.xp, a.residual ? q.rp : 0, q.dyp, out.dxp, a.dresidual ? out.drp : 0}, {x, dy, a.residual, dx, a.dresidual}, 4);
     const bool whole = d.Cg % vec == 0;
-    const TdcNormSlice sl = tdc_norm_slice(d, dt, vec, true, 1);
+    const TdcNormSlice sl = tdc_norm_slice(d, size, vec, true, 1);
     if (sl.held) {
         const int rows = tdc_norm_resident_rows(d, sl.slices);
         TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, TDC_FOR_SLICE(sl, tdc_norm_held(V, sizeof(T), true), false, THREADS, HELD, {

@@ -14,20 +14,10 @@
 #include <algorithm>
 #include <initializer_list>
 
+#include "tdc_norm_choice.h"
 #include "tdc_typed.h"
 
-constexpr int TDC_NORM_THREADS = 512;    // of the kernels that run over chunks
-constexpr int TDC_NORM_MAX_C = 8192;     // per-channel pairs of a workgroup fill at most 64 KiB of LDS
 constexpr int TDC_NORM_UNROLL = 4;       // pixels that a thread has in flight
-// Chunks of an image that every workgroup of the second kernel combines for itself.  More than that are combined by a kernel in
-// between: 224x224x64 in fp16, 196 chunks, 16.5 us without it and 14.3 with it; at 64 chunks the two are even.
-constexpr int TDC_NORM_PARTS = 64;
-
-struct TdcNormDims {
-    int B, P, C, G, Cg;     // P pixels to an image, Cg channels to a group
-    int chunk_px, chunks;
-    float eps;
-};
 
 struct tdc_norm_plan {
     tdc_norm_shape shape;
@@ -38,23 +28,6 @@ struct tdc_norm_plan {
     float2 *sums;        // [tdc_norm_sum_rows][C]: backward, sums of d and d xhat over some images or chunks
     size_t ws_bytes;
 };
-
-// Backward, the workgroups to a channel leave a row of sums each, to be added up for dgamma and dbeta: some 512 rows.  Resident,
-// every row is of some images; over chunks, there are as many rows to every chunk as this many images at a time make.
-constexpr int TDC_NORM_SUM_ROWS = 512;
-inline int tdc_norm_resident_rows(const TdcNormDims &d, int slices) { return std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / slices)); }
-inline int tdc_norm_chunk_images(const TdcNormDims &d) { return std::min(d.B, std::max(1, TDC_NORM_SUM_ROWS / d.chunks)); }
-inline size_t tdc_norm_sum_rows(const TdcNormDims &d)
-{
-    return std::max<size_t>((size_t)tdc_norm_chunk_images(d) * d.chunks, tdc_norm_resident_rows(d, 1));
-}
-
-// Pixels of chunk i of an image.
-__host__ __device__ inline int tdc_chunk_len(const TdcNormDims &d, int i)
-{
-    const int left = d.P - i * d.chunk_px;
-    return left < d.chunk_px ? left : d.chunk_px;
-}
 
 // How a workgroup's threads lie over `nv` pieces of a pixel.
 struct TdcNormLanes {
@@ -353,62 +326,6 @@ inline int tdc_norm_vec(int dtype, int C, std::initializer_list<int64_t> pitches
 }
 
 // ---- the resident form
-
-// Pieces of x that a thread holds at most.  Forward, two workgroups of 512 threads to a compute unit have 128 registers a thread:
-// 64 values of fp32, 32 of 16 bits that have to be converted.  Backward, where d is held too, in fp32, it is one with 256.
-__host__ __device__ constexpr int tdc_norm_held(int V, int size, bool backward) { return backward ? 8 : (V >= 4 && size == 2 ? 8 : 16); }
-
-// A workgroup takes `width` channels, whole groups and whole pieces, of an image; `slices` of them to an image.
-struct TdcNormSlice {
-    int width, slices, threads, held;    // held: pieces to a thread; 0: the image does not fit
-};
-
-// The narrowest slices (whole groups, whole pieces, multiples of `multiple`) are widened to a line of 128 bytes of a pixel, or 64
-// backward, and until there are no more than 1024 of them, as long as 512 threads hold them and 256 workgroups are left.  A line
-// that several workgroups share comes from memory once all the same: they run on the same XCD (tdc_norm_place).  Measured,
-// forward, fp32, 28x28x512, 32 images: 16 channels 21.8 us, 32 17.8; 28x28x128 in bf16, 32 images: 8 channels 9.6, 16 8.8, 32,
-// with 128 workgroups, 9.8; 7x7x512, 256 images: 16 channels 30.9 us, 64 and 128 11.9.  Backward, 14x14x1024 in bf16, 32 images:
-// 64 bytes 16.5, 128 18.9.  1024 threads lose everywhere (28x28x512, 32 images, 32 channels: 26.5; no second workgroup that reads
-// while one writes) but where slices below 64 bytes of a tensor larger than the L2s can be wider by them: 56x56x256, 32 images:
-// 8 channels 41.5 us, 16 38.9.
-inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int dtype, int V, bool backward, int multiple)
-{
-    const int size = tdc_dtype_bytes(dtype), most = tdc_norm_held(V, size, backward), line = backward ? 64 : 128;
-    int unit = d.Cg;
-    while ((unit % V || unit % multiple) && unit < d.C) unit += d.Cg;
-    if (unit > d.C || d.C % unit) unit = d.C;
-    auto held = [&](int width, int threads) {
-        const int nv = width / V;
-        return nv <= threads && width / d.Cg <= threads ? (d.P + threads / nv - 1) / (threads / nv) : 1 << 30;
-    };
-    auto next = [&](int width) {
-        do width += unit;
-        while (width < d.C && d.C % width);
-        return width;
-    };
-    auto fits = [&](int width) { return held(width, 512) <= most; };
-    auto groups = [&](int width) { return (int64_t)d.B * (d.C / width); };
-    if (!fits(unit)) return TdcNormSlice{};
-    int width = unit;
-    for (int w = next(width); w <= d.C && (width * size < line || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
-    if (!backward && width * size < 64 && (int64_t)d.B * d.P * d.C * size > (32 << 20)) {
-        const int w = next(width);
-        if (w <= d.C && held(w, 1024) <= most) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
-    }
-    const int threads = held(width, 256) <= 4 ? 256 : 512;
-    if (!backward && groups(width) * threads > 0xffffffffll) return TdcNormSlice{};   // a launch counts its threads in 32 bits
-    return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
-}
-
-// Whether the forward kernels store y past the L2's replacement: where workgroups write half lines or more of a tensor larger
-// than an XCD's L2 at about the same time, in pieces of 8 bytes or more.  28x28x512 in bf16, 32 images, 64 bytes to a slice: 18.4
-// us otherwise, 14.6 so.  But 56x56x256 in fp32, 32 images, where a compute unit has one workgroup of 1024 threads, with 64 bytes
-// to a slice 38.5 otherwise, 47.7 so; 56x56x64 in fp32, one image: 7.9 and 8.3.
-inline bool tdc_norm_streams(const TdcNormDims &d, int dtype, int V, const TdcNormSlice &sl)
-{
-    const int size = tdc_dtype_bytes(dtype);
-    return sl.threads != 1024 && (sl.held ? sl.width : d.C) * size >= 64 && V * size >= 8 && (double)d.B * d.P * d.C * size > 4e6;
-}
 
 // Workgroup id -> (image, slice): the ids that one XCD gets, 8 apart, are neighbours.
 __device__ __forceinline__ void tdc_norm_place(int id, int total, int slices, int &b, int &slice)

@@ -1,0 +1,55 @@
+"""Group norm at the ends of what it takes: the largest images, values that are no numbers, launches that differ from call to call.
+
+Tolerances as in test_gpu_norm.py: E = 2^-24 to a rounding, counted below where a thread merges or adds up more than there."""
+import pytest
+import torch
+
+import mx4_reference as R
+import norm_choice
+from test_gpu_norm import _layer
+
+pytestmark = pytest.mark.gpu
+E = R.E24
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def _over(got, want, bound, dtype):
+    """How far |got - want| passes the bound and half a step of dtype, on the GPU; both [n]."""
+    return float(((got.double() - want).abs() - bound - (want.abs() + bound) * R.HALF[dtype]).max())
+
+
+def test_an_image_next_to_2_31_pixels():
+    """46340 x 46341 pixels, whose number added to a chunk's passes 2^31.  A thread has 4096 of them.  Forward it merges them by
+    fours: 1024 roundings of the mean, and ten of differences that count less and less (the sum of 1/n, 8): 1200 E of the largest
+    value with the levels behind.  Backward it adds them up one after another: 4096 additions, and under 200 behind those."""
+    H, W = 46340, 46341
+    c = norm_choice.chunks((1, H, W, 1, 1), 2)
+    assert c["chunks"] == 1024 and norm_choice.slices((1, H, W, 1, 1), 2, 1)["held"] == 0
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, dy = (torch.empty((1, H, W, 1), device="cuda", dtype=BF16).normal_(generator=g) for _ in range(2))
+    gamma, beta = torch.tensor([1.25], device="cuda"), torch.tensor([-0.5], device="cuda")
+    gn = _layer(1, H, W, 1, 1, "none", BF16)
+    stats = gn.new_stats()
+    y = gn(x, gamma, beta, stats=stats)
+    dx, dgamma, dbeta, _ = gn.backward(x, dy, stats, gamma, beta)
+    pieces = lambda *ts: zip(*(t.reshape(-1).split(1 << 25) for t in ts))
+    n, top = H * W, float(x.abs().max())
+    mean = sum(float(a.double().sum()) for a, in pieces(x)) / n
+    var = sum(float((a.double() - mean).square().sum()) for a, in pieces(x)) / n
+    rstd = (var + 1e-5) ** -0.5
+    assert abs(float(stats[0]) - mean) <= 1200 * E * top and abs(float(stats[1]) - rstd) <= 1200 * E * rstd
+    w, b = float(gamma), float(beta)
+    for a, got in pieces(x, y):
+        xhat = (a.double() - mean) * rstd
+        assert _over(got, xhat * w + b, E * (1200 * (xhat.abs() + top * rstd) * w + 48 * abs(b)), BF16) <= 0
+    mean, rstd = float(stats[0]), float(stats[1])
+    s1 = s2 = a1 = a2 = 0.0
+    for a, d in pieces(x, dy):
+        d, t = d.double(), (a.double() - mean) * rstd * d.double()
+        s1, s2, a1, a2 = s1 + float(d.sum()), s2 + float(t.sum()), a1 + float(d.abs().sum()), a2 + float(t.abs().sum())
+    assert abs(float(dbeta) - s1) <= 4300 * E * a1 and abs(float(dgamma) - s2) <= 4300 * E * a2
+    for a, d, got in pieces(x, dy, dx):
+        xhat = (a.double() - mean) * rstd
+        want = rstd * w * (d.double() - s1 / n - xhat * s2 / n)
+        bound = rstd * w * E * (4310 * (a1 + xhat.abs() * a2) / n + 16 * (d.double().abs() + xhat.abs()))
+        assert _over(got, want, bound, BF16) <= 0
