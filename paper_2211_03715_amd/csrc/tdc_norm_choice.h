@@ -95,15 +95,16 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int size, int V, bool b
     };
     auto fits = [&](int width) { return held(width, 512) <= most; };
     auto groups = [&](int width) { return (int64_t)d.B * (d.C / width); };
+    auto launches = [&](int width, int threads) { return backward || groups(width) * threads <= 0xffffffffll; };   // a launch counts its threads in 32 bits
     if (!fits(unit)) return TdcNormSlice{};
     int width = unit;
     for (int w = next(width); w <= d.C && (width * size < line || groups(width) > 1024) && groups(w) >= 256 && fits(w); w = next(w)) width = w;
     if (!backward && width * size < 64 && (int64_t)d.B * d.P * d.C * size > (32 << 20)) {
         const int w = next(width);
-        if (w <= d.C && held(w, 1024) <= most) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
+        if (w <= d.C && held(w, 1024) <= most && launches(w, 1024)) return TdcNormSlice{w, d.C / w, 1024, held(w, 1024)};
     }
     const int threads = held(width, 256) <= 4 ? 256 : 512;
-    if (!backward && groups(width) * threads > 0xffffffffll) return TdcNormSlice{};   // a launch counts its threads in 32 bits
+    if (!launches(width, threads)) return TdcNormSlice{};
     return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
 }
 

@@ -26,3 +26,15 @@ def test_chunks_of_the_largest_images(H, W, batch):
 def test_no_image_of_that_size_stays_in_registers(H, W, backward):
     for C, groups, V in ((1, 1, 1), (2, 1, 2), (8, 2, 4), (8, 8, 1), (64, 32, 4), (8192, 8192, 4)):
         assert norm_choice.slices((1, H, W, C, groups), 4, V, backward)["held"] == 0
+
+
+# B, H, W, C, groups, bytes to an element, channels to an access: slices that would be widened by 1024 threads or not, and pass 2^32
+MANY = [(65535, 746, 1, 715, 715, 2, 1), (65535, 1, 130, 4020, 1340, 2, 1), (65535, 149, 1, 3536, 884, 2, 1), (65535, 1, 1, 8144, 509, 4, 4), (40000, 700, 1, 1430, 715, 2, 1)]
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_a_launch_has_fewer_than_2_32_threads(case):
+    B, *rest, size, V = case
+    cut = norm_choice.slices((B, *rest), size, V)
+    assert B * cut["slices"] * cut["threads"] < 2 ** 32
+    assert B * norm_choice.chunks((B, *rest), size)["chunks"] * 512 < 2 ** 32
