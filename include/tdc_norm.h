@@ -73,8 +73,8 @@ typedef struct tdc_norm_grad_args {
     int64_t x_pitch, residual_pitch, dy_pitch, dx_pitch, dresidual_pitch;
 } tdc_norm_grad_args;
 
-/* Gradients of tdc_group_norm, from the mean and rstd that it wrote.  With d = dy * act'(pre) (0 for TDC_ACT_RELU where
- * pre <= 0), g = d * gamma and m(.) the mean over a group of an image,
+/* Gradients of tdc_group_norm, from the mean and rstd that it wrote.  With d = dy * act'(pre) (TDC_ACT_RELU: dy where pre > 0, 0
+ * where pre <= 0 whatever dy is, NaN where pre is one), g = d * gamma and m(.) the mean over a group of an image,
  *     dx = rstd * (g - m(g) - xhat * m(g * xhat)),   dgamma[c] = sum d * xhat,   dbeta[c] = sum d,   dresidual = d.
  * dx: like x.  dgamma, dbeta: [C], overwritten, NULL where not wanted. */
 int tdc_group_norm_backward(tdc_norm_plan *plan, void *hip_stream, const void *x, const void *dy, const float *mean,

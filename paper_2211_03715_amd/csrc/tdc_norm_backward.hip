@@ -66,7 +66,7 @@ __device__ __forceinline__ void gradient(const Channels<V> &k, const TdcVec<T, V
             for (int v = 0; v < V; ++v) pre[v] += (float)res.v[v];
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) dd[v] *= q.act == TDC_ACT_RELU ? tdc_activate_grad<TDC_ACT_RELU>(pre[v]) : tdc_activate_grad<TDC_ACT_SILU>(pre[v]);
+        for (int v = 0; v < V; ++v) dd[v] = q.act == TDC_ACT_RELU ? tdc_activate_back<TDC_ACT_RELU>(dd[v], pre[v]) : tdc_activate_back<TDC_ACT_SILU>(dd[v], pre[v]);
     }
 }
 

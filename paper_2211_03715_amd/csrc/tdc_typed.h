@@ -106,15 +106,15 @@ template <int V> __device__ __forceinline__ void tdc_activate_all(int act, float
     }
 }
 
-// act'(v)
-template <int ACT> __device__ __forceinline__ float tdc_activate_grad(float v)
+// The gradient d of act(v) as that of v.  ReLU chooses: 0 where v <= 0 even for an infinite d, and a NaN of v stays one.
+template <int ACT> __device__ __forceinline__ float tdc_activate_back(float d, float v)
 {
-    if constexpr (ACT == TDC_ACT_RELU) return v > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == TDC_ACT_RELU) return v > 0.f ? d : (v != v ? v : 0.f);
     if constexpr (ACT == TDC_ACT_SILU) {
         const float s = tdc_sigmoid(v);
-        return s * (1.f + v * (1.f - s));
+        return d * (s * (1.f + v * (1.f - s)));
     }
-    return 1.f;
+    return d;
 }
 
 // ---- lanes of a wavefront, without a trip through LDS

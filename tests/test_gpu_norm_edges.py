@@ -6,7 +6,7 @@ import torch
 
 import mx4_reference as R
 import norm_choice
-from test_gpu_norm import _layer
+from test_gpu_norm import _inputs, _layer
 
 pytestmark = pytest.mark.gpu
 E = R.E24
@@ -53,3 +53,43 @@ def test_an_image_next_to_2_31_pixels():
         want = rstd * w * (d.double() - s1 / n - xhat * s2 / n)
         bound = rstd * w * E * (4310 * (a1 + xhat.abs() * a2) / n + 16 * (d.double().abs() + xhat.abs()))
         assert _over(got, want, bound, BF16) <= 0
+
+
+# one workgroup holds the image or a slice of it; an image in chunks
+@pytest.mark.parametrize("shape", [(2, 8, 8, 32, 4), (2, 150, 201, 16, 4)], ids=["resident", "chunks"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+def test_relu_chooses_gradients(shape, dtype):
+    """An infinite dy behind a closed ReLU is as good as 0 there; a NaN before a ReLU reaches the gradients that its value enters,
+    and no others."""
+    B, H, W, C, G = shape
+    assert (norm_choice.slices(shape, 4 if dtype is F32 else 2, 4, backward=True)["held"] > 0) == (H == 8)
+    x, gamma, beta, res, g = _inputs(B, H, W, C, dtype, residual=False, seed=3)
+    res = torch.randn((B, H, W, C), generator=g).to(dtype)
+    dy = torch.randn((B, H, W, C), generator=g).to(dtype)
+    res[1, 5, 3, 9] = -100                                    # closed
+    res[0, 2, 2, 6] = 100                                     # open
+    gn = _layer(B, H, W, C, G, "relu", dtype)
+    stats = gn.new_stats()
+    args = (x.cuda(), gamma.cuda(), beta.cuda())
+    grads = lambda dy, res: [t.cpu() for t in gn.backward(args[0], dy.cuda(), stats, *args[1:], residual=res.cuda())]
+    gn(*args, residual=res.cuda(), stats=stats)
+    dy[1, 5, 3, 9] = 0
+    want = grads(dy, res)
+    assert all(bool(torch.isfinite(t).all()) for t in want) and float(want[3][1, 5, 3, 9]) == 0
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        dy[1, 5, 3, 9] = bad
+        assert all(torch.equal(a, b) for a, b in zip(grads(dy, res), want))
+    dy[1, 5, 3, 9] = 0
+    for where in ((1, 5, 3, 9), (0, 2, 2, 6)):
+        holed = res.clone()
+        holed[where] = float("nan")
+        b, c = where[0], where[3]
+        group = slice(c // (C // G) * (C // G), (c // (C // G) + 1) * (C // G))
+        y = gn(*args, residual=holed.cuda()).cpu()
+        assert bool(torch.isnan(y[where])) and int(torch.isnan(y).sum()) == 1
+        dx, dgamma, dbeta, dres = grads(dy, holed)
+        for got, good, at, count in ((dx, want[0], (b, slice(None), slice(None), group), H * W * C // G), (dgamma, want[1], c, 1), (dbeta, want[2], c, 1),
+                                     (dres, want[3], where, 1)):
+            nan = torch.isnan(got)
+            assert bool(nan[at].all()) and int(nan.sum()) == count
+            assert torch.equal(got[~nan], good[~nan])
