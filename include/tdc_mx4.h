@@ -11,7 +11,7 @@
  *
  * Products sum in fp32 on the matrix cores that multiply such blocks directly.  As in tdc.h the calls only enqueue work on
  * `hip_stream`, allocate nothing and may be captured; codes must be 16-byte aligned, the other pointers to their elements.  Rows
- * may have up to 2^30 values.
+ * may have up to 2^30 values; what is more than a launch can cover, see each call, is TDC_ERR_UNSUPPORTED.
  * Outputs must not overlap inputs.  Calls without a plan run on the calling thread's CURRENT device, which must be the
  * stream's and the tensors'.
  */
@@ -28,11 +28,11 @@ extern "C" {
 #endif
 
 /* codes, scales <- the rows of x: [rows] of `cols` values of dtype TDC_F32 / F16 / BF16, `pitch` elements apart (0: cols).
- * rows = 0 is accepted and does nothing. */
+ * rows = 0 is accepted and does nothing.  TDC_ERR_UNSUPPORTED for more than 2^31 - 128 blocks, rows * ceil(cols/32). */
 int tdc_mx4_quantize(void *hip_stream, const void *x, int dtype, int64_t rows, int64_t cols, int64_t pitch, uint8_t *codes,
                      uint8_t *scales);
 
-/* y <- the values of codes and scales, rounded to dtype (fp16: values beyond its range become infinite). */
+/* y <- the values of codes and scales, rounded to dtype (fp16: values beyond its range become infinite).  The same limit. */
 int tdc_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *y,
                        int dtype, int64_t pitch);
 
@@ -45,15 +45,17 @@ typedef struct tdc_mx4_epilogue {
 } tdc_mx4_epilogue;
 
 /* y[M][N] = A[M][K] B[N][K]^T: both operands in rows of K values in 4 bits; y is stored in `dtype`.
- * M = 0 is accepted and does nothing.  TDC_ERR_UNSUPPORTED for N over 2^24. */
+ * M = 0 is accepted and does nothing.  TDC_ERR_UNSUPPORTED for N over 2^24, or when ceil(M/256) * ceil(N/256) reaches 2^23 (some
+ * 2^39 outputs). */
 int tdc_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                    const uint8_t *b_scales, int32_t M, int32_t N, int32_t K, void *y, int dtype,
                    const tdc_mx4_epilogue *epilogue);
 
 /* A 1x1 convolution on channels-last images with weights in 4 bits: x [batch][H][W][C] -> y [batch][Ho][Wo][N], with
  * Ho = ceil(H/stride), Wo = ceil(W/stride); output (i, j) reads input (i*stride, j*stride).  x_pitch: elements from one input
- * pixel to the next (0: C; else at least C).  TDC_ERR_UNSUPPORTED for an unknown dtype, for N over 2^24, or when batch*H*W, or
- * batch*Ho*Wo*N / 32, reaches 2^31. */
+ * pixel to the next (0: C; else at least C).  TDC_ERR_UNSUPPORTED for an unknown dtype, for N over 2^24, when batch*H*W reaches
+ * 2^31, or when the output's pixels, px = batch*Ho*Wo, pass 2^29 - 32, ceil(px/256) * ceil(N/256) reaches 2^23, or
+ * px * ceil(C/32) passes 2^31 - 128. */
 typedef struct tdc_mx4_shape {
     int32_t batch, H, W, C, N, stride;
     int32_t dtype;                /* of x, y and residual */

@@ -106,12 +106,8 @@ bool row_vectors(int dtype, int64_t cols, int64_t pitch, const void *p)
     return cols % v == 0 && pitch % v == 0 && tdc_aligned_to(p, 16);
 }
 
-// Workgroups of a launch along x; 0 where there are too many.
-unsigned blocks_for(int64_t items, int64_t per_block)
-{
-    const int64_t n = (items + per_block - 1) / per_block;
-    return n > 0x7fffffff / 256 ? 0u : (unsigned)n;
-}
+// Workgroups of a launch along x, for at most TDC_MX4_MAX_BLOCKS blocks.
+unsigned workgroups_for(int64_t blocks, int per_workgroup) { return (unsigned)((blocks + per_workgroup - 1) / per_workgroup); }
 
 hipError_t launch_quantize(hipStream_t s, const void *x, int dtype, const TdcMx4Rows &rows, int64_t n_rows, int cols, int64_t pitch, uint8_t *codes, uint8_t *scales)
 {
@@ -120,8 +116,7 @@ hipError_t launch_quantize(hipStream_t s, const void *x, int dtype, const TdcMx4
     const bool vectors = row_vectors(dtype, cols, pitch, x);
     TDC_FOR_DTYPE(dtype, T, {
         constexpr int V = 16 / sizeof(T);
-        const unsigned grid = blocks_for(total, 32 * V);   // 1024 pieces of V
-        if (!grid) return hipErrorInvalidValue;
+        const unsigned grid = workgroups_for(total, 32 * V);   // 1024 pieces of V
         if (vectors) tdc_mx4_quantize_lanes<T, V, true><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, TdcMx4Div(nb), pitch, codes, scales);
         else tdc_mx4_quantize_lanes<T, V, false><<<grid, 256, 0, s>>>((const T *)x, rows, total, cols, TdcMx4Div(nb), pitch, codes, scales);
     });
@@ -176,7 +171,7 @@ int tdc_mx4_quantize(void *hip_stream, const void *x, int dtype, int64_t rows, i
     if (pitch == 0) pitch = cols;
     if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
     if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(x, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
-    if (rows > INT64_MAX / 64 / tdc_mx4_blocks((int)cols) || !blocks_for(rows * tdc_mx4_blocks((int)cols), 128)) return TDC_ERR_UNSUPPORTED;
+    if (rows > TDC_MX4_MAX_BLOCKS / tdc_mx4_blocks((int)cols)) return TDC_ERR_UNSUPPORTED;
     return launch_quantize((hipStream_t)hip_stream, x, dtype, TdcMx4Rows::all(), rows, (int)cols, pitch, codes, scales) == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
@@ -188,14 +183,13 @@ int tdc_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint8_t *sc
     if (rows < 0 || cols < 1 || pitch < cols) return TDC_ERR_BAD_SHAPE;
     if (!tdc_known_dtype(dtype) || cols > TDC_MX4_MAX_COLS || !tdc_aligned_to(codes, 16) || !tdc_aligned_to(y, tdc_dtype_bytes(dtype))) return TDC_ERR_UNSUPPORTED;
     const int nb = tdc_mx4_blocks((int)cols);
-    if (rows > INT64_MAX / 64 / nb) return TDC_ERR_UNSUPPORTED;
+    if (rows > TDC_MX4_MAX_BLOCKS / nb) return TDC_ERR_UNSUPPORTED;
     const int64_t total = rows * nb;
-    if (!blocks_for(total, 128)) return TDC_ERR_UNSUPPORTED;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool vectors = row_vectors(dtype, cols, pitch, y);
     TDC_FOR_DTYPE(dtype, T, {
         constexpr int V = 16 / sizeof(T);
-        const unsigned grid = blocks_for(total, 32 * V);
+        const unsigned grid = workgroups_for(total, 32 * V);
         if (vectors) tdc_mx4_dequantize_lanes<T, V, true><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, TdcMx4Div(nb), pitch, (T *)y);
         else tdc_mx4_dequantize_lanes<T, V, false><<<grid, 256, 0, s>>>(codes, scales, total, (int)cols, TdcMx4Div(nb), pitch, (T *)y);
     });
@@ -229,7 +223,7 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS || s.N > TDC_MX4_MAX_OUT) return TDC_ERR_UNSUPPORTED;
     if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
     const int64_t rows = s.batch * Ho * Wo;
-    if (!tdc_mx4_product_fits((int)rows, s.N) || !blocks_for(rows * tdc_mx4_blocks(s.C), 128)) return TDC_ERR_UNSUPPORTED;
+    if (rows > TDC_MX4_MAX_ROWS || !tdc_mx4_product_fits(rows, s.N) || rows > TDC_MX4_MAX_BLOCKS / tdc_mx4_blocks(s.C)) return TDC_ERR_UNSUPPORTED;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || device < 0 || device >= ndev) return TDC_ERR_HIP;
     DeviceGuard guard(device);

@@ -55,8 +55,12 @@ inline bool tdc_mx4_vec(const TdcMx4Product &q, int dtype)
     return q.N % (16 / tdc_dtype_bytes(dtype)) == 0 && tdc_aligned_to(q.y, 16) && tdc_aligned_to(q.epi.residual, 16) && tdc_aligned_to(q.epi.bias, 16);
 }
 
-// Whether the kernels' grids cover M x N outputs.
-inline bool tdc_mx4_product_fits(int64_t M, int64_t N) { return ((M + 31) / 32) * ((N + 31) / 32) < 0x7fffffff / 256; }
+// A launch counts its threads in 32 bits.  Workgroups of 256 threads quantise 128 blocks at least, or have 32 rows of a convolution;
+// those of 512 have 256 x 256 outputs, or, in smaller tiles and by rows, launches are small.
+constexpr int64_t TDC_MX4_MAX_WORKGROUPS = (1 << 24) - 1;
+constexpr int64_t TDC_MX4_MAX_BLOCKS = 128 * TDC_MX4_MAX_WORKGROUPS;
+constexpr int64_t TDC_MX4_MAX_ROWS = 32 * TDC_MX4_MAX_WORKGROUPS;
+inline bool tdc_mx4_product_fits(int64_t M, int64_t N) { return ((M + 255) / 256) * ((N + 255) / 256) <= TDC_MX4_MAX_WORKGROUPS / 2; }
 
 hipError_t tdc_launch_mx4_product(const TdcMx4Product &q, int dtype, hipStream_t s);
 

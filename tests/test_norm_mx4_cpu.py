@@ -121,3 +121,19 @@ def test_more_outputs_than_2_to_the_24_are_refused():
     lib, plan = B.load(), ctypes.c_void_p()
     assert lib.tdc_mx4_matmul(None, P, P, P, P, 1, (1 << 24) + 1, 32, P, 0, None) == B.TDC_ERR_UNSUPPORTED
     assert lib.tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(_mx4(N=(1 << 24) + 1)), 0) == B.TDC_ERR_UNSUPPORTED and not plan.value
+
+
+def test_the_limits_that_the_header_states():
+    """Refused right above them; right below, what is refused is a device that is not there."""
+    lib, plan = B.load(), ctypes.c_void_p()
+    q, d = lib.tdc_mx4_quantize, lib.tdc_mx4_dequantize
+    for rows, cols in ((2 ** 31 - 127, 1), (2 ** 31 - 127, 32), (2 ** 30 - 63, 33), (2 ** 6, 2 ** 30), (2 ** 62, 2 ** 30)):
+        assert q(None, P, 2, rows, cols, 0, P, P) == B.TDC_ERR_UNSUPPORTED and d(None, P, P, rows, cols, P, 2, 0) == B.TDC_ERR_UNSUPPORTED, (rows, cols)
+    for M, N in ((2 ** 31 - 255, 1), (2 ** 30, 257), (2 ** 22, 2 ** 17), (2 ** 23, 2 ** 16)):
+        assert lib.tdc_mx4_matmul(None, P, P, P, P, M, N, 32, P, 0, None) == B.TDC_ERR_UNSUPPORTED, (M, N)
+    make = lambda **kw: lib.tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(_mx4(**kw)), 1 << 20)
+    for above in (dict(H=2 ** 29 - 31, W=1), dict(H=2 ** 15, W=2 ** 16), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16), dict(H=2 ** 14, W=2 ** 13, C=481)):
+        assert make(**above) == B.TDC_ERR_UNSUPPORTED and not plan.value, above
+    for below in (dict(H=2 ** 29 - 32, W=1), dict(H=2 ** 31 - 2, W=1, stride=5), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16 - 256), dict(H=2 ** 14, W=2 ** 13, C=480),
+                  dict(batch=64, H=224, W=224, C=64, N=4096, dtype=2)):
+        assert make(**below) == B.TDC_ERR_HIP and not plan.value, below
