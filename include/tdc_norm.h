@@ -44,7 +44,9 @@ typedef struct tdc_norm_plan tdc_norm_plan;   /* opaque, library-owned */
 int tdc_norm_plan_create(tdc_norm_plan **out, const tdc_norm_shape *shape, int device);
 int tdc_norm_plan_destroy(tdc_norm_plan *plan);                    /* NULL is accepted */
 size_t tdc_norm_plan_workspace_bytes(const tdc_norm_plan *plan);   /* device bytes owned */
-int tdc_norm_plan_kernel_count(const tdc_norm_plan *plan);         /* launches per tdc_group_norm call */
+/* Launches of a tdc_group_norm and of a tdc_group_norm_mx4 call on 16-byte aligned tensors without gaps. */
+int tdc_norm_plan_kernel_count(const tdc_norm_plan *plan);
+int tdc_norm_plan_mx4_kernel_count(const tdc_norm_plan *plan);
 
 /* Optional arguments.  A NULL tdc_norm_args, or zero in a field, is the default.
  * A pitch is the number of ELEMENTS from one pixel to the next (0: C; otherwise at least C), so a tensor may be a slice of the

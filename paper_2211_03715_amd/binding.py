@@ -44,7 +44,7 @@ EXPORTS = ["tdc_plan_create", "tdc_plan_create_tuned", "tdc_plan_pack_weights", 
            "tdc_select_tuning", "tdc_launch_null", "tdc_plan_pack_dense", "tdc_conv_dense", "tdc_select_ranks",
            "tdc_conv_tucker2_ex", "tdc_conv_dense_ex", "tdc_hosvd_tucker2", "tdc_admm_project",
            "tdc_conv_tucker2_static", "tdc_model_terms", "tdc_plan_status", "tdc_plan_set_wait_limit", "tdc_plan_waits_given_up",
-           "tdc_norm_plan_create", "tdc_norm_plan_destroy", "tdc_norm_plan_workspace_bytes", "tdc_norm_plan_kernel_count",
+           "tdc_norm_plan_create", "tdc_norm_plan_destroy", "tdc_norm_plan_workspace_bytes", "tdc_norm_plan_kernel_count", "tdc_norm_plan_mx4_kernel_count",
            "tdc_group_norm", "tdc_group_norm_mx4", "tdc_group_norm_backward",
            "tdc_mx4_quantize", "tdc_mx4_dequantize", "tdc_mx4_matmul", "tdc_mx4_plan_create", "tdc_mx4_plan_destroy",
            "tdc_mx4_plan_workspace_bytes", "tdc_mx4_plan_kernel_count", "tdc_mx4_plan_pack", "tdc_conv_mx4", "tdc_conv_mx4_quantized"]
@@ -184,7 +184,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     i64 = ctypes.c_int64
     norm_shape, mx4_shape = ctypes.POINTER(tdc_norm_shape), ctypes.POINTER(tdc_mx4_shape)
     norm_args, grad_args, mx4_epi = ctypes.POINTER(tdc_norm_args), ctypes.POINTER(tdc_norm_grad_args), ctypes.POINTER(tdc_mx4_epilogue)
-    for name, args in (("tdc_norm_plan_create", [ctypes.POINTER(vp), norm_shape, ip]), ("tdc_norm_plan_destroy", [vp]), ("tdc_norm_plan_kernel_count", [vp]),
+    for name, args in (("tdc_norm_plan_create", [ctypes.POINTER(vp), norm_shape, ip]), ("tdc_norm_plan_destroy", [vp]), ("tdc_norm_plan_kernel_count", [vp]), ("tdc_norm_plan_mx4_kernel_count", [vp]),
                        ("tdc_group_norm", [vp] * 6 + [norm_args]), ("tdc_group_norm_mx4", [vp] * 7 + [norm_args]),
                        ("tdc_group_norm_backward", [vp] * 11 + [grad_args]),
                        ("tdc_mx4_quantize", [vp, vp, ip, i64, i64, i64, vp, vp]), ("tdc_mx4_dequantize", [vp, vp, vp, i64, i64, vp, ip, i64]),
@@ -484,6 +484,10 @@ def tdc_norm_plan_workspace_bytes(plan) -> int:
 
 def tdc_norm_plan_kernel_count(plan) -> int:
     return int(load().tdc_norm_plan_kernel_count(plan))
+
+
+def tdc_norm_plan_mx4_kernel_count(plan) -> int:
+    return int(load().tdc_norm_plan_mx4_kernel_count(plan))
 
 
 def make_norm_args(residual=None, mean=None, rstd=None, x_pitch=0, residual_pitch=0, y_pitch=0) -> tdc_norm_args:

@@ -220,13 +220,16 @@ class TuckerNormBottleneck(TuckerBottleneck):
     def _norms(self):
         return [n for n in (self.normp, self.norm1, self.norm2, self.norm3) if n is not None]
 
+    def _norm_kernels(self):
+        return [n.kernel_count(quantized=n is self.norm2) for n in self._norms()]
+
     def kernels(self) -> int:
         # conv3 takes its rows quantised: one launch
-        return sum(n.kernel_count() for n in self._norms()) + sum(c.kernel_count() for c in self._convs() if c is not self.conv3) + 1
+        return sum(self._norm_kernels()) + sum(c.kernel_count() for c in self._convs() if c is not self.conv3) + 1
 
     def describe(self) -> str:
         head = "shortcut 1x1: 4 bits | " if self.projection else ""
-        return head + "1x1: 4 bits | 3x3: %s | 1x1: 4 bits | group norm: %s kernels" % (self.conv2.describe(), "+".join(str(n.kernel_count()) for n in self._norms()))
+        return head + "1x1: 4 bits | 3x3: %s | 1x1: 4 bits | group norm: %s kernels" % (self.conv2.describe(), "+".join(map(str, self._norm_kernels())))
 
     def close(self) -> None:
         for c in self._convs() + self._norms():

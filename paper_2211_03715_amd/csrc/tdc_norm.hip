@@ -316,6 +316,9 @@ int validate(const tdc_norm_shape &s)
 
 int64_t pitch_or(int64_t pitch, int C) { return pitch ? pitch : C; }
 
+// Of a forward call on aligned tensors without gaps.
+int launches(const tdc_norm_plan *p, bool mx4) { return tdc_norm_launches(p->dims, tdc_dtype_bytes(p->shape.dtype), tdc_norm_vec(p->shape.dtype, p->dims.C, {}, {}), mx4); }
+
 }  // namespace
 
 extern "C" {
@@ -361,12 +364,9 @@ int tdc_norm_plan_destroy(tdc_norm_plan *p)
 
 size_t tdc_norm_plan_workspace_bytes(const tdc_norm_plan *p) { return p ? p->ws_bytes : 0; }
 
-int tdc_norm_plan_kernel_count(const tdc_norm_plan *p)
-{
-    if (!p) return 0;
-    const int V = tdc_norm_vec(p->shape.dtype, p->dims.C, {}, {});
-    return tdc_norm_slice(p->dims, tdc_dtype_bytes(p->shape.dtype), V, false, 1).held ? 1 : p->dims.chunks > TDC_NORM_PARTS ? 3 : 2;
-}
+int tdc_norm_plan_kernel_count(const tdc_norm_plan *p) { return p ? launches(p, false) : 0; }
+
+int tdc_norm_plan_mx4_kernel_count(const tdc_norm_plan *p) { return p ? launches(p, true) : 0; }
 
 }  // extern "C"
 
@@ -388,8 +388,8 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
     const NormIn in{x, a.residual, gamma, beta, xp, rp, p->shape.act};
     const int vx = tdc_norm_vec(dt, d.C, {xp}, {x});
     const int V0 = y ? tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0, yp}, {x, a.residual, y}) : tdc_norm_vec(dt, d.C, {xp, a.residual ? rp : 0}, {x, a.residual});
-    const bool lanes = codes && d.C % 32 == 0 && V0 * size == 16;     // blocks of 4-bit values over neighbouring lanes
-    const TdcNormSlice sl = y || lanes ? tdc_norm_slice(d, size, V0, false, lanes ? 32 : 1) : TdcNormSlice{};
+    const bool lanes = codes && tdc_norm_block_lanes(d, size, V0);
+    const TdcNormSlice sl = tdc_norm_forward_slice(d, size, V0, codes != nullptr);
     const NormOut out{y, codes, scales, yp, a.mean, a.rstd, y && tdc_norm_streams(d, size, V0, sl)};
     const bool whole = d.Cg % V0 == 0, whole_x = d.Cg % vx == 0;
     const dim3 grid(d.chunks, d.B);

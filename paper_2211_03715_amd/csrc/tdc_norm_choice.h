@@ -108,6 +108,18 @@ inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int size, int V, bool b
     return TdcNormSlice{width, d.C / width, threads, held(width, threads)};
 }
 
+// A forward call's slice: of y, or of blocks of 4-bit values over neighbouring lanes, where C has whole blocks and accesses are 16 bytes.
+inline bool tdc_norm_block_lanes(const TdcNormDims &d, int size, int V) { return d.C % 32 == 0 && V * size == 16; }
+inline TdcNormSlice tdc_norm_forward_slice(const TdcNormDims &d, int size, int V, bool mx4)
+{
+    if (mx4 && !tdc_norm_block_lanes(d, size, V)) return TdcNormSlice{};
+    return tdc_norm_slice(d, size, V, false, mx4 ? 32 : 1);
+}
+inline int tdc_norm_launches(const TdcNormDims &d, int size, int V, bool mx4)
+{
+    return tdc_norm_forward_slice(d, size, V, mx4).held ? 1 : d.chunks > TDC_NORM_PARTS ? 3 : 2;
+}
+
 // Whether the forward kernels store y past the L2's replacement: where workgroups write half lines or more of a tensor larger
 // than an XCD's L2 at about the same time, in pieces of 8 bytes or more.  28x28x512 in bf16, 32 images, 64 bytes to a slice: 18.4
 // us otherwise, 14.6 so.  But 56x56x256 in fp32, 32 images, where a compute unit has one workgroup of 1024 threads, with 64 bytes

@@ -33,8 +33,9 @@ class GroupNorm:
         self.dev = torch.device("cuda", device)
         self.plan = B.tdc_norm_plan_create(B.tdc_norm_shape(batch, H, W, C, groups, dtype_code(self.dtype), self.act, eps), device)
 
-    def kernel_count(self) -> int:
-        return B.tdc_norm_plan_kernel_count(self.plan)
+    def kernel_count(self, quantized: bool = False) -> int:
+        """Launches of a call, or of one to quantized(), on aligned tensors without gaps."""
+        return B.tdc_norm_plan_mx4_kernel_count(self.plan) if quantized else B.tdc_norm_plan_kernel_count(self.plan)
 
     def new_stats(self):
         """Tensors that a call fills with the mean and 1/standard deviation of every group, for backward()."""

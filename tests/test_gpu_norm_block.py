@@ -130,3 +130,50 @@ def test_products_in_a_graph(M, N, K):
         torch.cuda.synchronize()
         p = mx4.quantize(xs[i])
         assert torch.equal(out[0], mx4.matmul(p, b, K, act="relu", dtype=torch.float16)) and torch.equal(out[1], mx4.dequantize(*p, K, dtype=torch.float16))
+
+
+def _kernel_nodes(enqueue):
+    """Kernels of a HIP graph that captures enqueue(): counted by the runtime."""
+    import ctypes
+
+    from paper_2211_03715_amd import binding as B
+    lib = B.load()                                     # its dependencies' functions are found through it
+    enqueue()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        enqueue()
+    handle, n = ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t()
+    assert lib.hipGraphGetNodes(handle, None, ctypes.byref(n)) == 0
+    nodes, kinds = (ctypes.c_void_p * n.value)(), []
+    assert lib.hipGraphGetNodes(handle, nodes, ctypes.byref(n)) == 0
+    for node in nodes:
+        kind = ctypes.c_int()
+        assert lib.hipGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
+        kinds.append(kind.value)
+    return kinds.count(0)                              # hipGraphNodeTypeKernel
+
+
+@pytest.mark.parametrize("shape", BLOCKS + [(32, 256, 64, 56, 56, 16, 16, 1, 256)], ids=lambda s: "x".join(map(str, s)))
+def test_a_block_counts_its_launches(shape):
+    """Against the kernels of its graph: at 56 x 56 the norm in 4 bits takes more launches than the same norm in fp32."""
+    blk, _ = _block(*shape)
+    x = torch.randn((shape[0], shape[3], shape[4], shape[1]), device="cuda")
+
+    def run():
+        blk.bind(x)
+        blk()
+
+    assert _kernel_nodes(run) == blk.kernels()
+    blk.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 56, 56, 64, 32), (32, 56, 56, 64, 32), (2, 7, 7, 512, 32), (2, 9, 9, 40, 5), (1, 224, 224, 64, 32), (8, 28, 28, 128, 32)], ids=lambda s: "x".join(map(str, s)))
+def test_a_norm_counts_its_launches(shape, dtype):
+    from paper_2211_03715_amd.norm import GroupNorm
+    gn = GroupNorm(*shape, dtype=dtype)
+    x = torch.randn(shape[:4], device="cuda").to(dtype)
+    y, q = torch.empty_like(x), gn.new_quantized()
+    assert _kernel_nodes(lambda: gn(x, y=y)) == gn.kernel_count()
+    assert _kernel_nodes(lambda: gn.quantized(x, out=q)) == gn.kernel_count(quantized=True)
