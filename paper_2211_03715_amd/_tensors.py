@@ -59,9 +59,10 @@ def stream_handle(stream, device) -> int:
 
 
 class on_stream:
-    """Outputs are allocated, and inputs kept, for the stream that the call runs on: with on_stream(stream, device, inputs): ..."""
+    """New outputs are allocated, and what the caller passes is kept, for the stream that the call runs on:
+    with on_stream(stream, device, tensors): ..."""
 
-    def __init__(self, stream, device, inputs):
+    def __init__(self, stream, device, tensors):
         self.context = None
         if stream is None:
             return
@@ -70,7 +71,7 @@ class on_stream:
         if ts.cuda_stream == torch.cuda.current_stream(device).cuda_stream:
             return
         if not torch.cuda.is_current_stream_capturing():
-            for t in inputs:
+            for t in tensors:
                 if t is not None:
                     t.record_stream(ts)
         self.context = torch.cuda.stream(ts)

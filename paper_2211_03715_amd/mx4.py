@@ -107,7 +107,7 @@ def matmul(a, b, K: int, bias=None, residual=None, act: str = "none", dtype=None
     bias_p = None if bias is None else expect(bias, "bias", (N,), torch.float32, dev).data_ptr()
     res_p = None if residual is None else expect(residual, "residual", lead + (N,), dtype, dev).data_ptr()
     epi = B.tdc_mx4_epilogue(bias_p, res_p, act_code(act))
-    with on_stream(stream, dev, tuple(a) + tuple(b) + (bias, residual)):
+    with on_stream(stream, dev, tuple(a) + tuple(b) + (bias, residual, y)):
         y = torch.empty(lead + (N,), device=dev, dtype=dtype) if y is None else expect(y, "y", lead + (N,), dtype, dev)
     _call(B.load().tdc_mx4_matmul, dev, stream, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(), _rows(lead), N, K, y.data_ptr(), code, ctypes.byref(epi),
           name="tdc_mx4_matmul")
@@ -180,7 +180,7 @@ class MX4Conv2d:
         if self._pack_event is not None:
             _order_after(self, stream if stream is not None else torch.cuda.current_stream(self.dev))
         if stream is not None:
-            with on_stream(stream, self.dev, (tuple(x) if isinstance(x, (tuple, list)) else (x,)) + (bias, residual)):
+            with on_stream(stream, self.dev, (tuple(x) if isinstance(x, (tuple, list)) else (x,)) + (bias, residual, y)):
                 y = torch.empty(self._out, device=self.dev, dtype=self.dtype) if y is None else y
         elif y is None:
             y = torch.empty(self._out, device=self.dev, dtype=self.dtype)

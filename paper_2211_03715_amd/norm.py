@@ -84,7 +84,7 @@ class GroupNorm:
         """Returns y (a new contiguous tensor unless given).  ``stats``: new_stats(), filled for backward()."""
         import torch
         if stream is not None:
-            with on_stream(stream, self.dev, (x, gamma, beta, residual)):
+            with on_stream(stream, self.dev, (x, gamma, beta, residual, y) + tuple(stats or ())):
                 y = torch.empty(self.shape, device=self.dev, dtype=self.dtype) if y is None else y
         elif y is None:
             y = torch.empty(self.shape, device=self.dev, dtype=self.dtype)
@@ -96,7 +96,7 @@ class GroupNorm:
 
     def quantized(self, x, gamma=None, beta=None, residual=None, out=None, stats=None, stream=None):
         """The same values in 4 bits, (codes, scales), quantised from float32 before any rounding to dtype."""
-        with on_stream(stream, self.dev, (x, gamma, beta, residual)):
+        with on_stream(stream, self.dev, (x, gamma, beta, residual) + tuple(out or ()) + tuple(stats or ())):
             out = out or self.new_quantized()
             fn, args = self._forward(x, gamma, beta, residual, stats, quantized=out)
             rc = fn(self.plan, stream_handle(stream, self.dev), *args)

@@ -177,3 +177,40 @@ def test_a_norm_counts_its_launches(shape, dtype):
     y, q = torch.empty_like(x), gn.new_quantized()
     assert _kernel_nodes(lambda: gn(x, y=y)) == gn.kernel_count()
     assert _kernel_nodes(lambda: gn.quantized(x, out=q)) == gn.kernel_count(quantized=True)
+
+
+def _stays(call, make):
+    """What make() gives call() stays the call's until the stream it runs on is done, although the caller drops it at once."""
+    side, busy = torch.cuda.Stream(), torch.empty(1 << 30, device="cuda")
+    kept = make()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):                            # some 10 ms of work before the call's
+            busy.fill_(1.0)
+    call(kept, side)
+    at = [t.data_ptr() for t in kept]
+    sizes = [(t.shape, t.dtype) for t in kept]
+    del kept
+    new = [torch.empty(s, device="cuda", dtype=d) for s, d in sizes for _ in range(3)]
+    assert not side.query(), "the stream was done too soon to tell"
+    assert not set(at) & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()
+
+
+def test_outputs_passed_in_are_kept_for_the_stream():
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.norm import GroupNorm
+    from paper_2211_03715_amd.workloads import Layer
+    x = torch.randn((2, 40, 40, 64), device="cuda")
+    gn, conv = GroupNorm(2, 40, 40, 64, 8), mx4.MX4Conv2d(Layer(2, 64, 96, 40, 40, 1, 1, 1, 1, 0))
+    conv.pack(torch.randn((64, 96), device="cuda"))
+    a, b = mx4.quantize(x.reshape(-1, 64)), mx4.quantize(torch.randn((96, 64), device="cuda"))
+    gn(x), gn.quantized(x), conv(x), mx4.matmul(a, b, 64)
+    y, z = lambda: torch.empty_like(x), lambda: torch.empty(conv.out_shape(), device="cuda")
+    _stays(lambda t, s: gn(x, y=t[0], stream=s), lambda: [y()])
+    _stays(lambda t, s: gn(x, stats=tuple(t), stream=s), lambda: list(gn.new_stats()))
+    _stays(lambda t, s: gn.quantized(x, out=tuple(t), stream=s), lambda: list(gn.new_quantized()))
+    _stays(lambda t, s: gn.quantized(x, stats=tuple(t), stream=s), lambda: list(gn.new_stats()))
+    _stays(lambda t, s: conv(x, t[0], stream=s), lambda: [z()])
+    _stays(lambda t, s: conv(a, t[0], stream=s), lambda: [z()])
+    _stays(lambda t, s: mx4.matmul(a, b, 64, y=t[0], stream=s), lambda: [z().reshape(-1, 96)])
