@@ -72,7 +72,7 @@ class on_stream:
             return
         if not torch.cuda.is_current_stream_capturing():
             for t in tensors:
-                if t is not None:
+                if t is not None and t.is_cuda:        # others are refused by the checks that follow
                     t.record_stream(ts)
         self.context = torch.cuda.stream(ts)
 

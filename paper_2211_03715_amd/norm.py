@@ -127,6 +127,8 @@ class GroupNorm:
         forward call's; dresidual is None without a residual."""
         import torch
         C = self.shape[3]
+        if stats is None:
+            raise ValueError("stats must be what the forward call filled")
         mean, rstd = self._stats(stats)
         with on_stream(stream, self.dev, (x, dy, gamma, beta, residual) + tuple(stats)):
             dx = torch.empty(self.shape, device=self.dev, dtype=self.dtype)

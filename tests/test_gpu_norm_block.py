@@ -214,3 +214,24 @@ def test_outputs_passed_in_are_kept_for_the_stream():
     _stays(lambda t, s: conv(x, t[0], stream=s), lambda: [z()])
     _stays(lambda t, s: conv(a, t[0], stream=s), lambda: [z()])
     _stays(lambda t, s: mx4.matmul(a, b, 64, y=t[0], stream=s), lambda: [z().reshape(-1, 96)])
+
+
+def test_refusals_with_a_stream():
+    """The same errors as without one."""
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.norm import GroupNorm
+    from paper_2211_03715_amd.workloads import Layer
+    side = torch.cuda.Stream()
+    x, w = torch.zeros((2, 4, 4, 64), device="cuda"), torch.zeros(64, device="cuda")
+    gn, conv = GroupNorm(2, 4, 4, 64, 8), mx4.MX4Conv2d(Layer(2, 64, 32, 4, 4, 1, 1, 1, 1, 0))
+    conv.pack(torch.zeros((64, 32), device="cuda"))
+    codes, scales = mx4.quantize(x.reshape(-1, 64))
+    stats = gn.new_stats()
+    for s in (None, side):
+        for call in (lambda: gn(x.cpu(), stream=s), lambda: gn(x, w.cpu(), stream=s), lambda: gn(x, y=x.cpu(), stream=s), lambda: gn(x, stats=tuple(t.cpu() for t in stats), stream=s),
+                     lambda: gn.quantized(x, out=(codes.cpu(), scales), stream=s), lambda: gn.backward(x, x.cpu(), stats, stream=s), lambda: gn.backward(x, x, None, stream=s),
+                     lambda: mx4.dequantize(codes, scales.cpu(), 64, stream=s), lambda: mx4.matmul((codes, scales), (codes, scales.cpu()), 64, stream=s),
+                     lambda: conv(x.cpu(), stream=s), lambda: conv(x, bias=torch.zeros(32), stream=s), lambda: conv(x, torch.zeros(conv.out_shape()), stream=s)):
+            with pytest.raises(ValueError):
+                call()
+    torch.cuda.synchronize()
