@@ -408,25 +408,26 @@ int forward(tdc_norm_plan *p, hipStream_t s, const void *x, const float *gamma, 
         })));
         return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
     }
+    hipError_t e = hipErrorInvalidValue;
     TDC_FOR_DTYPE(dt, T, {
         TDC_FOR_VEC(vx, T, V, {
             const int nv = d.C / V, rows = nv < TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
             const size_t lds = (size_t)rows * (whole_x ? nv : d.C) * sizeof(float2);
-            if (whole_x) tdc_norm_stats<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
-            else tdc_norm_stats<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, p->partial);
+            e = tdc_norm_launch(whole_x ? tdc_norm_stats<T, V, true> : tdc_norm_stats<T, V, false>, grid, lds, s, d, in, p->partial);
         });
+        if (e != hipSuccess) return TDC_ERR_HIP;
         const bool between = d.chunks > TDC_NORM_PARTS;
         if (between) tdc_norm_combine<<<dim3(d.G, d.B), 64, 0, s>>>(d, p->partial, p->whole);
         const float4 *sums = between ? p->whole : p->partial;
         const int parts = between ? 1 : d.chunks;
         TDC_FOR_VEC(V0, T, V, {
             const size_t lds = d.G * sizeof(float2);
-            if (y) tdc_norm_apply<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
-            else if (!lanes) tdc_norm_apply_blocks<T, V><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
-            else if constexpr (V * sizeof(T) == 16) tdc_norm_apply<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, in, out, sums, parts);
+            if (y) e = tdc_norm_launch(tdc_norm_apply<T, V, false>, grid, lds, s, d, in, out, sums, parts);
+            else if (!lanes) e = tdc_norm_launch(tdc_norm_apply_blocks<T, V>, grid, lds, s, d, in, out, sums, parts);
+            else if constexpr (V * sizeof(T) == 16) e = tdc_norm_launch(tdc_norm_apply<T, V, true>, grid, lds, s, d, in, out, sums, parts);
         });
     });
-    return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    return e == hipSuccess && hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }
 
 }  // namespace

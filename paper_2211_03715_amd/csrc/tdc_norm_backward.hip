@@ -280,7 +280,7 @@ template <typename T, int V, bool WHOLE>
 __global__ __launch_bounds__(TDC_NORM_THREADS) void tdc_norm_grad_sums(TdcNormDims d, GradIn q, float2 *__restrict__ partial, float2 *__restrict__ sums)
 {
     constexpr int U = TDC_NORM_UNROLL / 2;
-    extern __shared__ float2 items[];                      // rows * C, twice where a pixel takes several sweeps
+    extern __shared__ float2 items[];                      // rows * C
     const int nv = d.C / V, chunk = blockIdx.x, len = tdc_chunk_len(d, chunk);
     const TdcNormLanes t(nv, TDC_NORM_THREADS);
     const int used = min(t.rows, len);
@@ -436,21 +436,22 @@ extern "C" int tdc_group_norm_backward(tdc_norm_plan *p, void *hip_stream, const
     }
     const int images = tdc_norm_chunk_images(d);
     float2 *partial = reinterpret_cast<float2 *>(p->partial);
+    hipError_t e = hipErrorInvalidValue;
     TDC_FOR_DTYPE(dt, T, TDC_FOR_VEC4(vec, V, {
         const int nv = d.C / V, rows = nv < TDC_NORM_THREADS ? TDC_NORM_THREADS / nv : 1;
         const size_t lds = (size_t)rows * d.C * sizeof(float2);
         const dim3 grid(d.chunks, images);
-        if (whole) tdc_norm_grad_sums<T, V, true><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
-        else tdc_norm_grad_sums<T, V, false><<<grid, TDC_NORM_THREADS, lds, s>>>(d, q, partial, sums);
+        e = tdc_norm_launch(whole ? tdc_norm_grad_sums<T, V, true> : tdc_norm_grad_sums<T, V, false>, grid, lds, s, d, q, partial, sums);
+        if (e != hipSuccess) return TDC_ERR_HIP;
         const size_t lds_means = d.G * sizeof(float2);
         if (d.chunks > TDC_NORM_PARTS) {
             float2 *all = reinterpret_cast<float2 *>(p->whole);
             const unsigned wgs = (unsigned)(((size_t)d.B * d.G + 3) / 4);
             tdc_norm_grad_combine<<<wgs + weight_blocks, 256, 0, s>>>(d, partial, all, (int)wgs, sums, images * d.chunks, dgamma, dbeta);
-            tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks, TDC_NORM_THREADS, lds_means, s>>>(d, q, out, all, 1, nullptr, 0, nullptr, nullptr);
+            e = tdc_norm_launch(tdc_norm_grad_apply<T, V>, (unsigned)d.B * d.chunks, lds_means, s, d, q, out, all, 1, (const float2 *)nullptr, 0, (float *)nullptr, (float *)nullptr);
         } else {
-            tdc_norm_grad_apply<T, V><<<(unsigned)d.B * d.chunks + weight_blocks, TDC_NORM_THREADS, lds_means, s>>>(d, q, out, partial, d.chunks, sums, images * d.chunks, dgamma, dbeta);
+            e = tdc_norm_launch(tdc_norm_grad_apply<T, V>, (unsigned)d.B * d.chunks + weight_blocks, lds_means, s, d, q, out, partial, d.chunks, sums, images * d.chunks, dgamma, dbeta);
         }
     }));
-    return hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
+    return e == hipSuccess && hipGetLastError() == hipSuccess ? TDC_OK : TDC_ERR_HIP;
 }

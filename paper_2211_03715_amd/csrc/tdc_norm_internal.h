@@ -327,6 +327,14 @@ inline int tdc_norm_vec(int dtype, int C, std::initializer_list<int64_t> pitches
 
 // ---- the resident form
 
+// A launch of `fn` with dynamic LDS, which has to be allowed before a first one where it is much: up to 64 KiB for C near 8192.
+template <typename... P, typename... A> hipError_t tdc_norm_launch(void (*fn)(P...), dim3 grid, size_t lds, hipStream_t s, A... args)
+{
+    const hipError_t e = tdc_allow_lds((const void *)fn, lds);
+    if (e == hipSuccess) fn<<<grid, TDC_NORM_THREADS, lds, s>>>(args...);
+    return e;
+}
+
 // Workgroup id -> (image, slice): the ids that one XCD gets, 8 apart, are neighbours.
 __device__ __forceinline__ void tdc_norm_place(int id, int total, int slices, int &b, int &slice)
 {

@@ -93,3 +93,28 @@ def test_relu_chooses_gradients(shape, dtype):
             nan = torch.isnan(got)
             assert bool(nan[at].all()) and int(nan.sum()) == count
             assert torch.equal(got[~nan], good[~nan])
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 3, 8191, 1), (2, 1, 1, 8190, 2), (1, 1, 4200, 8192, 8192)], ids=lambda s: "x".join(map(str, s)))
+def test_launches_with_64_kib_of_lds_as_a_streams_first(shape):
+    """The widest pixels in chunks, whose kernels take up to 68 KiB of LDS, captured before any such call ran."""
+    B, H, W, C, G = shape
+    assert norm_choice.slices(shape, 2, 1 if C % 2 else 2 if C % 4 else 4, backward=True)["held"] == 0
+    xs = [torch.empty((B, H, W, C), device="cuda", dtype=BF16).normal_(generator=torch.Generator(device="cuda").manual_seed(s)) for s in (1, 2)]
+    dy, gamma, beta = xs[1] * 0.5, torch.full((C,), 1.5, device="cuda"), torch.full((C,), 0.25, device="cuda")
+    gn = _layer(B, H, W, C, G, "silu", BF16)
+    stats, static = gn.new_stats(), torch.zeros_like(xs[0])
+
+    def both(x):
+        return (gn(x, gamma, beta, stats=stats),) + gn.quantized(x, gamma, beta) + gn.backward(x, dy, stats, gamma, beta)[:3]
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(static)
+    for i in (0, 1, 0):
+        static.copy_(xs[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, both(xs[i]))), i
+        torch.cuda.synchronize()
