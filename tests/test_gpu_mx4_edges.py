@@ -77,3 +77,81 @@ def test_a_product_with_2_33_outputs(room):
     some = torch.tensor([0, 1, 255, 256, 32767, 32768, 50001, M - 1])
     want, err = _product(R.values(a[0][some], a[1][some], K), R.values(*b, K), None, None, "none", K)
     R.assert_within(y[some.cuda()], want, err, BF16, "y")
+
+
+# ---- every kernel that a convolution can choose
+
+def _values(q, C):
+    """R.values on the GPU."""
+    codes, scales = q
+    n = torch.stack((codes & 15, codes >> 4), -1).reshape(scales.shape + (32,)).long()
+    v = R.VALUES.to(codes.device)[n % 8] * (1 - 2 * (n // 8).double()) * torch.pow(2.0, scales.double() - 127)[..., None]
+    return v.reshape(scales.shape[:-1] + (-1,))[..., :C]
+
+
+def _way(batch, H, W, C, N, stride):
+    """As tdc_mx4_internal.h chooses: products in large tiles; a workgroup to 32 rows and 64 columns, eight wavefronts along k; or a
+    workgroup to 32 rows, its wavefronts at 64 columns each."""
+    rows = batch * ((H - 1) // stride + 1) * ((W - 1) // stride + 1)
+    if rows >= 4096 and N >= 1024 and C >= 1024:
+        return "large"
+    return "few" if -(-rows // 32) * -(-N // 64) <= 512 else "many"
+
+
+# batch, H, W, C, N, stride, extra pixel pitch: ragged columns, pixels in whole pieces and not, every second or third pixel, gaps between
+# pixels, k beyond what LDS holds at a time (8192)
+WAYS = [("many", (8, 60, 60, 100, 150, 1, 0)), ("many", (8, 61, 59, 104, 151, 2, 0)), ("many", (2, 100, 100, 264, 330, 1, 8)), ("many", (1, 130, 131, 33, 65, 1, 3)), ("many", (8, 90, 88, 40, 1000, 3, 1)),
+        ("many", (32, 28, 28, 128, 512, 1, 0)), ("many", (1, 73, 76, 8232, 190, 1, 0)), ("many", (1, 73, 76, 8225, 190, 1, 0)),
+        ("large", (16, 17, 19, 1056, 1040, 1, 0)), ("large", (8, 47, 45, 1030, 1028, 2, 2)), ("large", (4, 33, 33, 1024, 1041, 1, 0)), ("large", (5, 30, 29, 2048, 1024, 1, 8)),
+        ("few", (1, 4, 4, 9000, 64, 1, 0)), ("few", (1, 9, 9, 2056, 70, 2, 8)), ("few", (5, 9, 9, 65, 33, 1, 0))]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("way,shape", WAYS, ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else s)
+def test_every_way_of_a_convolution(way, shape, dtype):
+    """Against the definition in 64 bits on the blocks that quantize() gives, which test_gpu_mx4.py compares bit for bit."""
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.workloads import Layer
+    batch, H, W, C, N, stride, extra = shape
+    assert _way(*shape[:6]) == way
+    act = ("none", "relu", "silu")[(H + C + N) % 3]
+    print("[case] conv", way, shape, dtype, act, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(C * 7 + N)
+    randn = lambda *s: torch.randn(s, device="cuda", generator=g)
+    wide = randn(batch, H, W, C + extra).to(dtype)
+    x, Wt, bias = wide[..., :C], randn(C, N) * C ** -0.5, randn(N)
+    conv = mx4.MX4Conv2d(Layer(batch, C, N, H, W, 1, 1, 1, stride, 0), dtype=dtype, x_pitch=C + extra)
+    conv.pack(Wt)
+    out = conv.out_shape()
+    extras = {"bias": bias, "residual": randn(*out).to(dtype) if (N + H) % 2 else None, "act": act}
+    q = mx4.quantize(x)
+    y, z = conv(x, torch.full(out, float("nan"), device="cuda", dtype=dtype), **extras), conv(q, torch.full(out, float("nan"), device="cuda", dtype=dtype), **extras)
+    xv = _values(tuple(t[:, ::stride, ::stride].contiguous() for t in q), C).reshape(-1, C)
+    wv = _values(mx4.quantize(Wt.t().contiguous()), C)
+    res = None if extras["residual"] is None else extras["residual"].reshape(-1, N)
+    want, err = _product(xv, wv, bias, res, act, C)
+    for got in (y, z):
+        R.assert_within(got.reshape(-1, N), want.cpu(), err.cpu(), dtype, "y")
+    assert torch.equal(conv(x, **extras), y)
+
+
+@pytest.mark.parametrize("way,shape", [("many", (2, 100, 100, 96, 200)), ("large", (4, 33, 33, 1024, 1040)), ("few", (2, 5, 5, 96, 200))], ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else s)
+def test_what_is_no_number_stays_in_its_pixel(way, shape):
+    """An infinity or a NaN makes its pixel's outputs NaN whichever kernel runs, a pixel of zeros gives the bias."""
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.workloads import Layer
+    B, H, W, C, N = shape
+    assert _way(*shape, 1) == way
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn((B, H, W, C), device="cuda", generator=g)
+    bias = torch.randn(N, device="cuda", generator=g)
+    conv = mx4.MX4Conv2d(Layer(B, C, N, H, W, 1, 1, 1, 1, 0))
+    conv.pack(torch.randn((C, N), device="cuda", generator=g))
+    good = conv(x, bias=bias)
+    x[0, 1, 2, C - 1], x[1, 3, 0, 5], x[1, 4, 4], x[0, 4, 3, 40] = float("inf"), -float("inf"), 0, float("nan")
+    for got in (conv(x, bias=bias), conv(mx4.quantize(x), bias=bias)):
+        nan = torch.isnan(got)
+        assert all(bool(nan[at].all()) for at in ((0, 1, 2), (1, 3, 0), (0, 4, 3))) and int(nan.sum()) == 3 * N
+        assert torch.equal(got[1, 4, 4], bias)
+        nan[1, 4, 4] = True
+        assert torch.equal(got[~nan], good[~nan])          # the same products in the same order
