@@ -58,6 +58,16 @@ def stream_handle(stream, device) -> int:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def torch_stream(stream, device):
+    """torch's stream object on `device` for None (its current stream), a raw handle (0: the default stream) or a torch stream."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if isinstance(stream, int):
+        return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return stream
+
+
 class on_stream:
     """New outputs are allocated, and what the caller passes is kept, for the stream that the call runs on:
     with on_stream(stream, device, tensors): ..."""
@@ -67,7 +77,7 @@ class on_stream:
         if stream is None:
             return
         import torch
-        ts = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) and stream else torch.cuda.default_stream(device) if isinstance(stream, int) else stream
+        ts = torch_stream(stream, device)
         if ts.cuda_stream == torch.cuda.current_stream(device).cuda_stream:
             return
         if not torch.cuda.is_current_stream_capturing():

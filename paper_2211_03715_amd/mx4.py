@@ -9,8 +9,8 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stream_handle
-from .layer import _order_after, _torch_stream
+from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stream_handle, torch_stream
+from .layer import _order_after
 
 
 def _call(fn, device, stream, *args, name):
@@ -151,7 +151,7 @@ class MX4Conv2d:
         expect(W, "W", W.shape, torch.float32, self.dev)
         with on_stream(stream, self.dev, (W,)):
             B.tdc_mx4_plan_pack(self.plan, W, stream_handle(stream, self.dev))
-        ts = torch.cuda.current_stream(self.dev) if stream is None else _torch_stream(stream)
+        ts = torch_stream(stream, self.dev)
         self._pack_event = ts.record_event()
         self._ordered = {ts.cuda_stream}
 
@@ -178,7 +178,7 @@ class MX4Conv2d:
         """y = act(conv(x) + bias[n] + residual)."""
         import torch
         if self._pack_event is not None:
-            _order_after(self, stream if stream is not None else torch.cuda.current_stream(self.dev))
+            _order_after(self, torch_stream(stream, self.dev))
         if stream is not None:
             with on_stream(stream, self.dev, (tuple(x) if isinstance(x, (tuple, list)) else (x,)) + (bias, residual, y)):
                 y = torch.empty(self._out, device=self.dev, dtype=self.dtype) if y is None else y
@@ -194,7 +194,7 @@ class MX4Conv2d:
         """A zero-argument launcher with the arguments marshalled once.  The tensors and the stream must outlive it."""
         import torch
         if self._pack_event is not None:
-            _order_after(self, stream if stream is not None else torch.cuda.current_stream(self.dev))
+            _order_after(self, torch_stream(stream, self.dev))
         fn, args = self._arguments(x, y, bias, residual, act)
         plan, handle = self.plan, ctypes.c_void_p(stream_handle(stream, self.dev))
         args = tuple(ctypes.c_void_p(a) if isinstance(a, int) else a for a in args)

@@ -137,3 +137,49 @@ def test_the_limits_that_the_header_states():
     for below in (dict(H=2 ** 29 - 32, W=1), dict(H=2 ** 31 - 2, W=1, stride=5), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16 - 256), dict(H=2 ** 14, W=2 ** 13, C=480),
                   dict(batch=64, H=224, W=224, C=64, N=4096, dtype=2)):
         assert make(**below) == B.TDC_ERR_HIP and not plan.value, below
+
+
+def test_raw_streams_belong_to_the_layers_device(monkeypatch):
+    """A handle means a stream of the layer's device, whichever is current: when weights are packed on it and when a call waits for that."""
+    import contextlib
+
+    from paper_2211_03715_amd import mx4
+    there = torch.device("cuda", 1)
+    made = []
+
+    class Stream:
+        def __init__(self, kind, handle, device):
+            self.kind, self.cuda_stream, self.device, self.waited = kind, handle, device, False
+            made.append(self)
+
+        def record_event(self):
+            return self                                # is its own event, never done
+
+        def query(self):
+            return False
+
+        def wait_event(self, event):
+            self.waited = True
+
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Stream("raw", handle, device))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream("default", 0, device))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream("current", 77, device))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    conv = mx4.MX4Conv2d.__new__(mx4.MX4Conv2d)
+    conv.plan, conv.dev, conv.dtype, conv._out = None, there, torch.float32, (1,)
+    conv.layer = type("Layer", (), dict(C=8, N=4))
+    conv._arguments = lambda *a: (lambda *b: B.TDC_OK, (None,))
+    monkeypatch.setattr(mx4, "expect", lambda *a: None)
+    monkeypatch.setattr(mx4, "on_stream", lambda *a: contextlib.nullcontext())
+    monkeypatch.setattr(mx4.B, "tdc_mx4_plan_pack", lambda *a: None)
+    y = torch.zeros(1)
+    for packed_on, kind in ((12345, "raw"), (0, "default")):
+        del made[:]
+        conv.pack(torch.zeros(8, 4), stream=packed_on)
+        conv(None, y=y, stream=54321)
+        conv.bind(None, None, stream=65432)
+        used = [s for s in made if s.kind != "current"]
+        assert [s.kind for s in used] == [kind, "raw", "raw"] and all(s.device == there for s in used) and [s.waited for s in used] == [False, True, True]
+    from paper_2211_03715_amd import _tensors
+    own = Stream("own", 5, there)
+    assert _tensors.torch_stream(own, there) is own and _tensors.torch_stream(None, there).device == there
