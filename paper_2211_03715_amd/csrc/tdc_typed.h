@@ -184,18 +184,12 @@ template <typename F> __device__ __forceinline__ void tdc_merge_lanes(int from, 
     if (from <= 32) f([](float v) { return tdc_rows32(v).x; }, [](float v) { return tdc_rows32(v).y; });
 }
 
-// The statements for a dtype with T its type, for an activation with the constant ACT, for V neighbours with the constant V.
+// The statements for a dtype with T its type, for V neighbours with the constant V.
 #define TDC_FOR_DTYPE(dtype, T, ...)                                  \
     do {                                                              \
         if ((dtype) == TDC_F32) { using T = float; __VA_ARGS__; }     \
         else if ((dtype) == TDC_F16) { using T = tdc_half; __VA_ARGS__; } \
         else { using T = tdc_bf16; __VA_ARGS__; }                     \
-    } while (0)
-#define TDC_FOR_ACT(act, ACT, ...)                                                              \
-    do {                                                                                        \
-        if ((act) == TDC_ACT_RELU) { constexpr int ACT = TDC_ACT_RELU; __VA_ARGS__; }           \
-        else if ((act) == TDC_ACT_SILU) { constexpr int ACT = TDC_ACT_SILU; __VA_ARGS__; }      \
-        else { constexpr int ACT = TDC_ACT_NONE; __VA_ARGS__; }                                 \
     } while (0)
 
 #define TDC_FOR_VEC(v, T, V, ...)                                                         \
