@@ -155,3 +155,45 @@ def test_what_is_no_number_stays_in_its_pixel(way, shape):
         assert torch.equal(got[1, 4, 4], bias)
         nan[1, 4, 4] = True
         assert torch.equal(got[~nan], good[~nan])          # the same products in the same order
+
+
+def test_the_binding_alone():
+    """Every function of the binding, on plans and tensors without the layers, gives what the layers give."""
+    from paper_2211_03715_amd import binding as B
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.norm import GroupNorm
+    from paper_2211_03715_amd.workloads import Layer
+    g = torch.Generator(device="cuda").manual_seed(11)
+    randn = lambda *s: torch.randn(s, device="cuda", generator=g)
+    n, H, C, N, G = 2, 9, 72, 40, 6
+    x, dy, res, gamma, beta, W, bias = randn(n, H, H, C), randn(n, H, H, C), randn(n, H, H, C), randn(C), randn(C), randn(C, N), randn(N)
+    gn, conv = GroupNorm(n, H, H, C, G, act="silu"), mx4.MX4Conv2d(Layer(n, C, N, H, H, 1, 1, 1, 1, 0))
+    conv.pack(W)
+    stats = gn.new_stats()
+    want = [gn(x, gamma, beta, residual=res, stats=stats), *gn.quantized(x, gamma, beta, residual=res)] + list(gn.backward(x, dy, stats, gamma, beta, residual=res))
+    norm = B.tdc_norm_plan_create(B.tdc_norm_shape(n, H, H, C, G, B.F32, B.ACT_SILU, 1e-5))
+    assert B.tdc_norm_plan_workspace_bytes(norm) > 0
+    assert B.tdc_norm_plan_kernel_count(norm) == gn.kernel_count() and B.tdc_norm_plan_mx4_kernel_count(norm) == gn.kernel_count(quantized=True)
+    y, (codes, scales), (mean, rstd) = torch.empty_like(x), gn.new_quantized(), gn.new_stats()
+    dx, dres, dgamma, dbeta = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    B.tdc_group_norm(norm, x, gamma, beta, y, B.make_norm_args(residual=res, mean=mean, rstd=rstd))
+    B.tdc_group_norm_mx4(norm, x, gamma, beta, codes, scales, B.make_norm_args(residual=res))
+    B.tdc_group_norm_backward(norm, x, dy, mean, rstd, gamma, beta, dx, dgamma, dbeta, B.make_norm_grad_args(residual=res, dresidual=dres))
+    assert all(torch.equal(a, b) for a, b in zip((y, codes, scales, dx, dgamma, dbeta, dres), want))
+    B.tdc_norm_plan_destroy(norm)
+
+    rows = x.reshape(-1, C)
+    q, w4 = mx4.quantize(rows), mx4.quantize(W.t().contiguous())
+    a, b, back, z = torch.empty_like(q[0]), torch.empty_like(q[1]), torch.empty_like(rows), torch.empty((rows.shape[0], N), device="cuda")
+    B.tdc_mx4_quantize(rows, B.F32, rows.shape[0], C, a, b)
+    B.tdc_mx4_dequantize(a, b, rows.shape[0], C, back, B.F32)
+    B.tdc_mx4_matmul(a, b, *w4, rows.shape[0], N, C, z, B.F32, B.make_mx4_epilogue(bias=bias, act=B.ACT_RELU))
+    assert torch.equal(a, q[0]) and torch.equal(b, q[1]) and torch.equal(back, mx4.dequantize(*q, C)) and torch.equal(z, mx4.matmul(q, w4, C, bias=bias, act="relu"))
+    plan = B.tdc_mx4_plan_create(B.tdc_mx4_shape(n, H, H, C, N, 1, B.F32, 0))
+    assert B.tdc_mx4_plan_workspace_bytes(plan) > 0 and B.tdc_mx4_plan_kernel_count(plan) == conv.kernel_count()
+    B.tdc_mx4_plan_pack(plan, W)
+    c, d = (torch.empty(conv.out_shape(), device="cuda") for _ in range(2))
+    B.tdc_conv_mx4(plan, x, c, B.make_mx4_epilogue(bias=bias))
+    B.tdc_conv_mx4_quantized(plan, a, b, d)
+    assert torch.equal(c, conv(x, bias=bias)) and torch.equal(d, conv(tuple(t.reshape(n, H, H, -1) for t in q)))
+    B.tdc_mx4_plan_destroy(plan)
