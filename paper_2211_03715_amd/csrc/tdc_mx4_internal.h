@@ -82,15 +82,20 @@ hipError_t tdc_launch_mx4_rows(const TdcMx4Product &q, const TdcMx4Source &src, 
 constexpr int TDC_MX4_MAX_COLS = 1 << 30;
 constexpr int TDC_MX4_MAX_OUT = 1 << 24;   // a lane's offset of some rows of y stays under 2^32 bytes
 
-// A convolution that the matrix cores bound rather than memory runs as quantisation and a product in large tiles.
+// A convolution that the matrix cores bound rather than memory runs as quantisation and a product in large tiles.  By rows and so, us:
+// bf16, 4096 rows, 1024 -> 1024 14.1 and 11.5, 2048 -> 2048 40.5 and 20.5, 512 -> 1024 9.5 and 9.7, 1024 -> 512 12.1 and 11.3;
+// 2048 rows, 512 -> 1024 7.1 and 9.1; 25088 rows, 1024 -> 1024 36.3 and 39.4, 2048 -> 1024 90.5 and 66.7; fp32, 4096 rows,
+// 1024 -> 1024 17.2 and 13.2; 25088 rows, 64.0 and 57.6.  Below the limits
+// either wins; long sums are better so from 2048 rows or 512 columns on (2048 rows, 2048 -> 2048 in bf16: 23.4 and 14.3).
 inline bool tdc_mx4_large(int64_t rows, int N, int K) { return rows >= 4096 && N >= 1024 && K >= 1024; }
 
 // Whether tdc_launch_mx4_rows gives a workgroup 32 rows and only 64 columns, eight wavefronts along k.
 inline bool tdc_mx4_few(int64_t rows, int N) { return (rows + 31) / 32 * ((N + 63) / 64) <= 512; }
 
-// Every one of those quantises its rows of x anew, which takes longer than a launch where they have over 192 KB: 64 rows,
-// 4096 -> 4096 in bf16 (262 KB) 17.4 us, with x quantised in a launch of its own 10.4; 1568 rows, 2048 -> 512 in fp32 (262 KB)
-// 21.1 and 13.7; 6272 rows, 512 -> 128 in fp32 (66 KB) 7.4 and 10.0.
+// Every one of those quantises its rows of x anew, which takes longer than a launch where they have over 192 KB.  On the way and in a
+// launch of its own: 64 rows, 4096 -> 4096 in bf16 (262 KB) 18.9 us and 12.1; 1568 rows, 2048 -> 512 in fp32 (262 KB) 20.8 and 13.4;
+// 49 such rows 9.4 and 8.8; in bf16 (131 KB) 1568 rows 16.5 and 12.3, 196 rows 10.2 and 9.0, but 1024 -> 256 in fp32 (131 KB), 196
+// rows, 6.6 and 8.1; 6272 rows, 512 -> 128 in fp32 (66 KB) 9.1 and 10.8.
 inline bool tdc_mx4_quantise_first(int64_t rows, int N, int K, int size) { return tdc_mx4_few(rows, N) && (double)(rows < 32 ? rows : 32) * K * size > 192e3; }
 
 #endif  // TDC_MX4_INTERNAL_H

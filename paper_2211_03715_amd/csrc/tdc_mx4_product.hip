@@ -17,9 +17,10 @@ hipError_t tdc_launch_mx4_product(const TdcMx4Product &given, int dtype, hipStre
 {
     TdcMx4Product q = given;
     q.vec = tdc_mx4_vec(q, dtype);
-    // Tiles of 256 x 256 where over half of the compute units get one (3300 x 2600 x 900, 143 of them: 16.2 us, in tiles of
-    // 128 x 128 18.1; 4096 x 2048 x 1024, 128 of them: 13.7 and 9.9), of 128 x 128 from 64 of those on; below that, and for few
-    // rows, every 32 rows and 64 columns by themselves (700 x 700 x 2048, 36 tiles of 128 x 128: 8.6 us by rows, 15.1 in tiles).
+    // Tiles of 256 x 256 where over half of the compute units get one (3300 x 2600 x 900, 143 of them: 15.9 us, in tiles of
+    // 128 x 128 18.4; 4096 x 2048 x 1024, 128 of them: 13.4 and 9.3; but 3200 x 2560 x 2048, 130 of them: 20.0 and 14.4), of
+    // 128 x 128 from 64 of those on; below that, and for few rows, every 32 rows and 64 columns by themselves (700 x 700 x 2048, 36
+    // tiles of 128 x 128: 9.4 us by rows, 15.2 in tiles).
     const int64_t large = up(q.M, 256) * up(q.N, 256), small = up(q.M, 128) * up(q.N, 128);
     if (q.M <= 64 || small < 64) return tdc_launch_mx4_rows(q, TdcMx4Source{nullptr, 0, 0}, dtype, nullptr, nullptr, s);
     const bool packed = q.nb % 16 == 0 && tdc_aligned_to(q.a_scales, 16) && tdc_aligned_to(q.b_scales, 16);

@@ -76,8 +76,8 @@ __device__ __forceinline__ void store_gradients(const Channels<V> &k, const Grad
     float o[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) o[v] = k.rstd[v] * (dd[v] * k.gamma[v] - m1[v] - xhat[v] * m2[v]);
-    // Past the L2's replacement where pieces are whole: 14x14x1024 in bf16, 32 images 26.0 us otherwise, 23.7 so; 56x56x256, from
-    // cold caches 62.2 and 56.7; a choice at run time cost 4 % of it.
+    // Past the L2's replacement where pieces are whole; 32 images, otherwise and so: 56x56x256 in fp32 106.6 us and 90.9, in bf16
+    // 61.8 and 57.5, 14x14x1024 18.1 and 17.9, 28x28x512 35.4 and 35.8; a choice at run time cost 4 %.
     auto store = [](T *p, const float (&f)[V]) {
         if constexpr (V == 4) tdc_store_stream<T, V>(p, f);
         else tdc_store<T, V>(p, f);

@@ -75,9 +75,11 @@ struct TdcNormSlice {
 // that several workgroups share comes from memory once all the same: they run on the same XCD (tdc_norm_place).  Measured,
 // forward, fp32, 28x28x512, 32 images: 16 channels 21.8 us, 32 17.8; 28x28x128 in bf16, 32 images: 8 channels 9.6, 16 8.8, 32,
 // with 128 workgroups, 9.8; 7x7x512, 256 images: 16 channels 30.9 us, 64 and 128 11.9.  Backward, 14x14x1024 in bf16, 32 images:
-// 64 bytes 16.5, 128 18.9.  1024 threads lose everywhere (28x28x512, 32 images, 32 channels: 26.5; no second workgroup that reads
-// while one writes) but where slices below 64 bytes of a tensor larger than the L2s can be wider by them: 56x56x256, 32 images:
-// 8 channels 41.5 us, 16 38.9.
+// 64 bytes 16.5, 128 18.9.  1024 threads lose (28x28x512, 32 images, 32 channels: 26.5; no second workgroup that reads while one
+// writes) but where slices below 64 bytes of a tensor larger than the L2s can be wider by them.  With 512 threads and with 1024, over
+// three sets of buffers in turn, fp32: 56x56x256, 16, 32 and 64 images 39.6 and 26.2 us, 65.1 and 54.9, 117.6 and 100.6; 32
+// images of 48x48x256 50.0 and 41.8, 56x56x128 36.0 and 25.0, 64x64x256 86.4 and 65.4, 80x80x64 48.3 and 32.0, but 48x48x128 16.8
+// and 17.0, 40x40x192 23.3 and 25.6; bf16: 56x56x256 50.4 and 38.3, 40x40x512 40.5 and 34.0.
 inline TdcNormSlice tdc_norm_slice(const TdcNormDims &d, int size, int V, bool backward, int multiple)
 {
     const int most = tdc_norm_held(V, size, backward), line = backward ? 64 : 128;
@@ -122,8 +124,9 @@ inline int tdc_norm_launches(const TdcNormDims &d, int size, int V, bool mx4)
 
 // Whether the forward kernels store y past the L2's replacement: where workgroups write half lines or more of a tensor larger
 // than an XCD's L2 at about the same time, in pieces of 8 bytes or more.  28x28x512 in bf16, 32 images, 64 bytes to a slice: 18.4
-// us otherwise, 14.6 so.  But 56x56x256 in fp32, 32 images, where a compute unit has one workgroup of 1024 threads, with 64 bytes
-// to a slice 38.5 otherwise, 47.7 so; 56x56x64 in fp32, one image: 7.9 and 8.3.
+// us otherwise, 14.6 so.  Not where a compute unit has one workgroup of 1024 threads: 32 images in fp32, otherwise and so,
+// 56x56x256 54.9 and 58.5, 64x64x256 65.4 and 78.1, 40x40x192 25.6 and 39.0, though 48x48x256 41.8 and 37.4; nor for small
+// tensors: 56x56x64 in fp32, one image, 7.9 and 8.3.
 inline bool tdc_norm_streams(const TdcNormDims &d, int size, int V, const TdcNormSlice &sl)
 {
     return sl.threads != 1024 && (sl.held ? sl.width : d.C) * size >= 64 && V * size >= 8 && (double)d.B * d.P * d.C * size > 4e6;

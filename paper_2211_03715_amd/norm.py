@@ -20,7 +20,8 @@ class GroupNorm:
     """y = act(group_norm(x) * gamma + beta + residual) on x [batch][H][W][C] with C/groups neighbouring channels to a group.
 
     x, residual and y are of ``dtype`` (float32, float16, bfloat16) and may be slices of the channels of wider pixels; gamma, beta
-    and the statistics are float32.  ``act``: "none", "relu" or "silu"."""
+    and the statistics are float32.  ``act``: "none", "relu" or "silu".  As with the other layers no call enters torch's graph of
+    gradients: a result does not require one, and backward() is called by the program."""
 
     def __init__(self, batch: int, H: int, W: int, C: int, groups: int, eps: float = 1e-5, act: str = "none", dtype=None, device: int = 0):
         import torch
