@@ -31,7 +31,7 @@ enum { TDC_F32 = 0, TDC_F16 = 1, TDC_BF16 = 2 };
 enum { TDC_ACT_NONE = 0, TDC_ACT_RELU = 1, TDC_ACT_SILU = 2 };
 
 /* batch 1..65535, H*W < 2^31, C 1..8192 and a multiple of groups, eps >= 0; else TDC_ERR_BAD_SHAPE (sizes that mean nothing) or
- * TDC_ERR_UNSUPPORTED (unknown dtype or act, C or batch too large). */
+ * TDC_ERR_UNSUPPORTED (unknown dtype or act, C, batch or H*W too large). */
 typedef struct tdc_norm_shape {
     int32_t batch, H, W, C, groups;
     int32_t dtype;                /* of x, y, residual and their gradients */

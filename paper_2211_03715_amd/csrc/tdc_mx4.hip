@@ -221,7 +221,7 @@ int tdc_mx4_plan_create(tdc_mx4_plan **out, const tdc_mx4_shape *shape, int devi
     if (s.x_pitch < s.C) return TDC_ERR_BAD_SHAPE;
     const int64_t Ho = (s.H - 1) / s.stride + 1, Wo = (s.W - 1) / s.stride + 1, lim = 0x7fffffff;
     if (!tdc_known_dtype(s.dtype) || s.C > TDC_MX4_MAX_COLS || s.N > TDC_MX4_MAX_OUT) return TDC_ERR_UNSUPPORTED;
-    if ((double)s.batch * s.H * s.W >= (double)lim) return TDC_ERR_UNSUPPORTED;
+    if ((double)s.batch * s.H * s.W > (double)lim) return TDC_ERR_UNSUPPORTED;
     const int64_t rows = s.batch * Ho * Wo;
     if (rows > TDC_MX4_MAX_ROWS || !tdc_mx4_product_fits(rows, s.N) || rows > TDC_MX4_MAX_BLOCKS / tdc_mx4_blocks(s.C)) return TDC_ERR_UNSUPPORTED;
     int ndev = 0;

@@ -52,6 +52,21 @@ def test_a_convolution_of_as_many_pixels_as_a_plan_takes(room):
         assert torch.equal(a.float(), 0.75 * b.float())
 
 
+def test_every_fifth_of_2_31_pixels(room):
+    """The largest image, one channel in and out; what is read lies up to 2^31 - 2 pixels in."""
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.workloads import Layer
+    n = 2 ** 31 - 1
+    x = torch.empty((1, n, 1, 1), device="cuda", dtype=BF16).normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    conv = mx4.MX4Conv2d(Layer(1, 1, 1, n, 1, 1, 1, 1, 5, 0), dtype=BF16)
+    conv.pack(torch.full((1, 1), 0.75, device="cuda"))
+    y, q = conv(x), mx4.quantize(x[:, ::5].contiguous())
+    v = mx4.dequantize(*q, 1, dtype=BF16)
+    assert y.shape == v.shape
+    for a, b in zip(y.reshape(-1).split(1 << 26), v.reshape(-1).split(1 << 26)):
+        assert torch.equal(a.float(), 0.75 * b.float())
+
+
 def test_a_convolution_with_more_than_2_33_outputs(room):
     """64 images of 224 x 224, 64 channels to 4096: 2^33.6 outputs of 16 bits.  Some pixels of each image are looked at."""
     from paper_2211_03715_amd import mx4

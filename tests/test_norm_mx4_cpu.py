@@ -134,7 +134,7 @@ def test_the_limits_that_the_header_states():
     make = lambda **kw: lib.tdc_mx4_plan_create(ctypes.byref(plan), ctypes.byref(_mx4(**kw)), 1 << 20)
     for above in (dict(H=2 ** 29 - 31, W=1), dict(H=2 ** 15, W=2 ** 16), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16), dict(H=2 ** 14, W=2 ** 13, C=481)):
         assert make(**above) == B.TDC_ERR_UNSUPPORTED and not plan.value, above
-    for below in (dict(H=2 ** 29 - 32, W=1), dict(H=2 ** 31 - 2, W=1, stride=5), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16 - 256), dict(H=2 ** 14, W=2 ** 13, C=480),
+    for below in (dict(H=2 ** 29 - 32, W=1), dict(H=2 ** 31 - 1, W=1, stride=5), dict(H=2 ** 12, W=2 ** 11, N=2 ** 16 - 256), dict(H=2 ** 14, W=2 ** 13, C=480),
                   dict(batch=64, H=224, W=224, C=64, N=4096, dtype=2)):
         assert make(**below) == B.TDC_ERR_HIP and not plan.value, below
 
