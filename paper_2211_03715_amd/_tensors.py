@@ -23,6 +23,13 @@ def act_code(act: str) -> int:
     return B.ACTS[act]
 
 
+def sizes(**named):
+    """Sizes that go to the library in 32 bits, which would silently be cut to them."""
+    for name, v in named.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError("%s must be below 2^31, not %d" % (name, v))
+
+
 def _refuse(t, name, shape, dtype, device):
     raise ValueError("%s must be %s %s on %s, not %s %s on %s" % (name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
 

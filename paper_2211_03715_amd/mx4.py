@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stream_handle, torch_stream
+from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, sizes, stream_handle, torch_stream
 from .layer import _order_after
 
 
@@ -103,13 +103,15 @@ def matmul(a, b, K: int, bias=None, residual=None, act: str = "none", dtype=None
     code, lead, b_lead, dev = dtype_code(dtype), _pair(*a, K, "a"), _pair(*b, K, "b"), a[0].device
     if len(b_lead) != 1 or b[0].device != dev:
         raise ValueError("b must hold rows [N][K] on a's device")
-    N = b_lead[0]
+    N, M = b_lead[0], _rows(lead)
+    if max(M, N, K) >> 31:
+        sizes(M=M, N=N, K=K)
     bias_p = None if bias is None else expect(bias, "bias", (N,), torch.float32, dev).data_ptr()
     res_p = None if residual is None else expect(residual, "residual", lead + (N,), dtype, dev).data_ptr()
     epi = B.tdc_mx4_epilogue(bias_p, res_p, act_code(act))
     with on_stream(stream, dev, tuple(a) + tuple(b) + (bias, residual, y)):
         y = torch.empty(lead + (N,), device=dev, dtype=dtype) if y is None else expect(y, "y", lead + (N,), dtype, dev)
-    _call(B.load().tdc_mx4_matmul, dev, stream, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(), _rows(lead), N, K, y.data_ptr(), code, ctypes.byref(epi),
+    _call(B.load().tdc_mx4_matmul, dev, stream, a[0].data_ptr(), a[1].data_ptr(), b[0].data_ptr(), b[1].data_ptr(), M, N, K, y.data_ptr(), code, ctypes.byref(epi),
           name="tdc_mx4_matmul")
     return y
 
@@ -127,6 +129,7 @@ class MX4Conv2d:
         self.plan = None
         if layer.K != 1 or layer.pad != 0:
             raise ValueError("a 4-bit convolution is 1x1 without padding")
+        sizes(**{k: getattr(layer, k) for k in ("batch", "H", "W", "C", "N", "stride")})
         self.layer, self.dtype = layer, dtype or torch.float32
         self.dev = torch.device("cuda", device)
         self.x_pitch = x_pitch or layer.C

@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, stream_handle
+from ._tensors import act_code, dtype_code, expect, on_stream, pixel_pitch, sizes, stream_handle
 
 
 def _float32():
@@ -26,6 +26,7 @@ class GroupNorm:
     def __init__(self, batch: int, H: int, W: int, C: int, groups: int, eps: float = 1e-5, act: str = "none", dtype=None, device: int = 0):
         import torch
         self.plan = None
+        sizes(batch=batch, H=H, W=W, C=C, groups=groups)
         self.dtype = dtype or torch.float32
         self.shape = (batch, H, W, C)
         self._blocks = -(-C // 32)

@@ -183,3 +183,32 @@ def test_raw_streams_belong_to_the_layers_device(monkeypatch):
     from paper_2211_03715_amd import _tensors
     own = Stream("own", 5, there)
     assert _tensors.torch_stream(own, there) is own and _tensors.torch_stream(None, there).device == there
+
+
+def test_sizes_beyond_32_bits_are_refused(monkeypatch):
+    """ctypes would hand the library their low 32 bits: a plan for 7 pixels where 2^32 + 7 were meant."""
+    from types import SimpleNamespace
+
+    from paper_2211_03715_amd import mx4, norm
+    reached = []
+    monkeypatch.setattr(B, "tdc_norm_plan_create", lambda *a: reached.append(a))
+    monkeypatch.setattr(B, "tdc_mx4_plan_create", lambda *a: reached.append(a))
+    for v in (2 ** 31, 2 ** 32 + 8):
+        for i in range(5):
+            args = [1, 8, 8, 8, 8]
+            args[i] = v
+            with pytest.raises(ValueError):
+                norm.GroupNorm(*args)
+        for name in ("batch", "H", "W", "C", "N", "stride"):
+            layer = SimpleNamespace(**dict(dict(batch=1, H=8, W=8, C=8, N=8, stride=1, K=1, pad=0), **{name: v}))
+            with pytest.raises(ValueError):
+                mx4.MX4Conv2d(layer)
+    # rows of a product: tensors that only say how large they are
+    monkeypatch.setattr(mx4, "_pair", lambda codes, scales, K, name: codes.shape[:-1])
+    large = SimpleNamespace(shape=(2 ** 16, 2 ** 16 + 1, 16), device="cuda:0")
+    small = SimpleNamespace(shape=(4, 16), device="cuda:0")
+    monkeypatch.setattr(mx4, "_call", lambda *a, **k: reached.append(a))
+    for a, b, K in ((large, small, 32), (small, small, 2 ** 32 + 32)):
+        with pytest.raises(ValueError):
+            mx4.matmul((a, a), (b, b), K)
+    assert not reached
