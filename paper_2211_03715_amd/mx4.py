@@ -199,11 +199,11 @@ class MX4Conv2d:
         if self._pack_event is not None:
             _order_after(self, torch_stream(stream, self.dev))
         fn, args = self._arguments(x, y, bias, residual, act)
-        plan, handle = self.plan, ctypes.c_void_p(stream_handle(stream, self.dev))
+        handle = ctypes.c_void_p(stream_handle(stream, self.dev))
         args = tuple(ctypes.c_void_p(a) if isinstance(a, int) else a for a in args)
 
         def launch():
-            rc = fn(plan, handle, *args)
+            rc = fn(self.plan, handle, *args)          # keeps the layer, and refuses once it is closed
             if rc:
                 raise B.TdcError(rc, "tdc_conv_mx4")
 

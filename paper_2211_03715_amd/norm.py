@@ -107,11 +107,11 @@ class GroupNorm:
         return out
 
     def _bound(self, fn, args, stream, name):
-        plan, handle = self.plan, ctypes.c_void_p(stream_handle(stream, self.dev))
+        handle = ctypes.c_void_p(stream_handle(stream, self.dev))
         args = tuple(ctypes.c_void_p(a) if isinstance(a, int) else a for a in args)
 
         def launch():
-            rc = fn(plan, handle, *args)
+            rc = fn(self.plan, handle, *args)          # keeps the layer, and refuses once it is closed
             if rc:
                 raise B.TdcError(rc, name)
 

@@ -212,3 +212,42 @@ def test_sizes_beyond_32_bits_are_refused(monkeypatch):
         with pytest.raises(ValueError):
             mx4.matmul((a, a), (b, b), K)
     assert not reached
+
+
+def test_launchers_keep_their_layer_and_refuse_once_it_is_closed(monkeypatch):
+    """A plan that went with its layer would be read after it was freed."""
+    import gc
+
+    from paper_2211_03715_amd import mx4, norm
+    destroyed = []
+    monkeypatch.setattr(B, "tdc_norm_plan_destroy", lambda plan: destroyed.append(plan.value))
+    monkeypatch.setattr(B, "tdc_mx4_plan_destroy", lambda plan: destroyed.append(plan.value))
+    monkeypatch.setattr(norm, "stream_handle", lambda *a: 0)
+    monkeypatch.setattr(mx4, "stream_handle", lambda *a: 0)
+    call = lambda plan, *a: B.TDC_ERR_NULL if plan is None else B.TDC_OK
+
+    def made(cls, number):
+        layer = cls.__new__(cls)
+        layer.plan, layer.dev = ctypes.c_void_p(number), torch.device("cuda", 0)
+        return layer
+
+    def conv(number):
+        layer = made(mx4.MX4Conv2d, number)
+        layer._pack_event, layer._arguments = None, lambda *a: (call, (None,))
+        return layer.bind(None, None), layer
+
+    def gn(number):
+        layer = made(norm.GroupNorm, number)
+        layer._forward = lambda *a, **k: (call, (None,))
+        return layer.bind(None, None), layer
+
+    for make, number in ((conv, 1), (gn, 2)):
+        launch = make(number)[0]
+        gc.collect()
+        assert number not in destroyed
+        launch()
+        launch, layer = make(10 + number)
+        layer.close()
+        assert destroyed[-1] == 10 + number
+        with pytest.raises(B.TdcError):
+            launch()
