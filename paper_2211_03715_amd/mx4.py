@@ -133,9 +133,9 @@ class MX4Conv2d:
         self.layer, self.dtype = layer, dtype or torch.float32
         self.dev = torch.device("cuda", device)
         self.x_pitch = x_pitch or layer.C
-        self._in, self._out = (layer.batch, layer.H, layer.W, layer.C), (layer.batch, (layer.H - 1) // layer.stride + 1, (layer.W - 1) // layer.stride + 1, layer.N)
         self._pack_event = None
         self.plan = B.tdc_mx4_plan_create(B.tdc_mx4_shape(layer.batch, layer.H, layer.W, layer.C, layer.N, layer.stride, dtype_code(self.dtype), self.x_pitch), device)
+        self._in, self._out = (layer.batch, layer.H, layer.W, layer.C), (layer.batch, (layer.H - 1) // layer.stride + 1, (layer.W - 1) // layer.stride + 1, layer.N)
 
     def out_shape(self):
         return self._out

@@ -251,3 +251,12 @@ def test_launchers_keep_their_layer_and_refuse_once_it_is_closed(monkeypatch):
         assert destroyed[-1] == 10 + number
         with pytest.raises(B.TdcError):
             launch()
+
+
+def test_a_stride_of_zero_is_the_plans_refusal():
+    from paper_2211_03715_amd import mx4
+    from paper_2211_03715_amd.workloads import Layer
+    for stride in (0, -1):
+        with pytest.raises(B.TdcError) as refused:
+            mx4.MX4Conv2d(Layer(1, 8, 8, 4, 4, 1, 1, 1, stride, 0))
+        assert refused.value.status == B.TDC_ERR_BAD_SHAPE
