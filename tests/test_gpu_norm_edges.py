@@ -118,3 +118,56 @@ def test_launches_with_64_kib_of_lds_as_a_streams_first(shape):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, both(xs[i]))), i
         torch.cuda.synchronize()
+
+
+# resident; chunks; chunks of pixels with more pieces than threads, several images to a workgroup
+GRADS = [(2, 8, 8, 32, 4), (2, 90, 110, 40, 5), (530, 1, 1, 8184, 8)]
+
+
+@pytest.mark.parametrize("extra,offset", [(0, 0), (8, 8), (16, 4), (3, 1)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape", GRADS, ids=lambda s: "x".join(map(str, s)))
+def test_gradients_into_slices_and_only_those_wanted(shape, dtype, extra, offset):
+    """tdc_group_norm_backward with dx and dresidual in wider pixels, whose rest stays as it was, and without gradients that are not
+    wanted: one statistic of the forward pass, dgamma or dbeta or neither, no dresidual, dresidual without a residual."""
+    from paper_2211_03715_amd import binding as B
+    from test_gpu_norm_paths import _backward_want
+    n, H, W, C, G = shape
+    g = torch.Generator(device="cuda").manual_seed(C)
+    randn = lambda *s: torch.randn(s, device="cuda", generator=g)
+    x, dy, res = (randn(n, H, W, C).to(dtype) for _ in range(3))
+    gamma, beta = 1 + 0.2 * randn(C), 0.2 * randn(C)
+    gn = _layer(n, H, W, C, G, "silu", dtype)
+    mean, rstd = gn.new_stats()
+    alone = gn.new_stats()
+    y = gn(x, gamma, beta, residual=res, stats=(mean, rstd))
+    for kw in (dict(mean=alone[0]), dict(rstd=alone[1])):
+        B.tdc_group_norm(gn.plan, x, gamma, beta, torch.empty_like(y), B.make_norm_args(residual=res, **kw))
+    assert torch.equal(alone[0], mean) and torch.equal(alone[1], rstd)
+    pitch = C + extra + offset
+    cut = lambda t: t[..., offset:offset + C]
+
+    def backward(dgamma=True, dbeta=True, dresidual=True, residual=True):
+        wide = [torch.full((n, H, W, pitch), 7.0, device="cuda", dtype=dtype) for _ in range(2)]
+        sums = [torch.full((C,), float("nan"), device="cuda") for _ in range(2)]
+        B.tdc_group_norm_backward(gn.plan, x, dy, mean, rstd, gamma, beta, cut(wide[0]), sums[0] if dgamma else None, sums[1] if dbeta else None,
+                                  B.make_norm_grad_args(residual=res if residual else None, dresidual=cut(wide[1]) if dresidual else None, dx_pitch=pitch, dresidual_pitch=pitch))
+        for t in wide:
+            assert bool((t[..., :offset] == 7).all()) and bool((t[..., offset + C:] == 7).all())
+        return [cut(wide[0])] + sums + [cut(wide[1])]
+
+    for residual in (True, False):
+        full = backward(residual=residual)
+        _, want = _backward_want(x, dy, (mean, rstd), gamma, beta, res if residual else None, "silu")
+        for t, (name, (v, err)) in zip(full, want.items()):
+            R.assert_within(t, v.cpu(), err.cpu(), F32 if name in ("dgamma", "dbeta") else dtype, name)
+        for kw in (dict(dgamma=False), dict(dbeta=False), dict(dgamma=False, dbeta=False), dict(dresidual=False)):
+            got = backward(residual=residual, **kw)
+            for t, whole, name in zip(got, full, ("dx", "dgamma", "dbeta", "dresidual")):
+                if kw.get(name, True):
+                    # without dresidual pieces may be wider, and sums in another order
+                    v, err = want[name]
+                    R.assert_within(t, v.cpu(), err.cpu(), F32 if name in ("dgamma", "dbeta") else dtype, name)
+                    assert "dresidual" in kw or torch.equal(t, whole), (kw, name)
+                else:
+                    assert bool((t == 7).all()) if name == "dresidual" else bool(torch.isnan(t).all())
